@@ -84,7 +84,8 @@ enum { A2ATS_F32 = 0, A2ATS_BF16 = 1 };                       /* element types o
 enum { A2ATS_W_NONE = 0, A2ATS_W_DIAG = 1, A2ATS_W_BLOCK = 2 }; /* encoder distortion              */
 enum { A2ATS_W_PREPARED = 0x100 };   /* flag for weight_mode, see a2ats_encode_prepare */
 enum { A2ATS_OP_ENCODE = 0, A2ATS_OP_LUT = 1, A2ATS_OP_SCORE_TOPK = 2, A2ATS_OP_ATTN = 3, A2ATS_OP_FIT = 4,
-       A2ATS_OP_SEED = 5 };
+       A2ATS_OP_SEED = 5, A2ATS_OP_BLOCK_TOPK = 6, A2ATS_OP_ATTN_KV8 = 7 };
+enum { A2ATS_I8 = 0, A2ATS_E4M3 = 1 };   /* formats of a cache held in 8 bits, see a2ats_kv8_append */
 
 int a2ats_version(void);
 const char* a2ats_status_string(int status);
@@ -96,6 +97,8 @@ size_t a2ats_lut_elems(const a2ats_dims* dims);
  * A2ATS_OP_ATTN and A2ATS_OP_SCORE_TOPK the figure covers every call with up to 64 sink tokens; a
  * call with more may need more and is refused with A2ATS_ERR_WORKSPACE if `ws` is too small. */
 size_t a2ats_workspace_bytes(const a2ats_dims* dims, int op, int32_t top_k, int32_t window);
+/* (A2ATS_OP_BLOCK_TOPK: covers every block size and both kinds of selection.  A2ATS_OP_ATTN_KV8: `top_k` is the number of
+ * selected tokens, n_sel * sel_size; both kinds of selection and any number of sinks.) */
 
 /*
  * Host helper: rotation tables for WRoPE (paper section 4.1, eq. "WRoPE"; section 2.1).
@@ -408,6 +411,106 @@ int a2ats_decode_select_shared(const a2ats_dims* dims, const float* keys, int32_
                                int32_t top_k, int32_t window, int32_t n_sink, const int32_t* seq_lens,
                                int32_t* topk_idx, int32_t* topk_count, float* topk_score, void* ws,
                                size_t ws_bytes, void* stream);
+
+/*
+ * A key/value cache cut into blocks of tokens.
+ *
+ * Three things go by blocks of `block` consecutive tokens of one sequence, 16, 32, 64 or 128 (block c holds the tokens
+ * c * block .. c * block + block - 1):
+ *   - keys and values in 8 bits with a scale for each block and KV head (a2ats_kv8_append writes them,
+ *     a2ats_sparse_attn_kv8 reads them; half the memory and bytes of bfloat16, a quarter of float32);
+ *   - bounds of a block's keys per dimension, and a selection of blocks by them (a2ats_block_topk), which needs no
+ *     codebook;
+ *   - attention over selected blocks.
+ * All memory is the caller's; the struct is read on the host during a call.  Pointers are 16-byte aligned but for the
+ * scales (4) and the page table (4).
+ *   contiguous (page_table NULL): "piece" below is [B][Hkv][ctx_stride / block]; ctx_stride is a multiple of block
+ *   paged: [n_pages][Hkv][page_size / block], token j of sequence b in page page_table[b][j / page_size], page_table
+ *     [dev, int32 B * ceil(ctx_stride / page_size)]; page_size: a power of two >= block.  Every page number that a token
+ *     below ctx_len / seq_lens reaches must be a valid page (not checked on the device), and no page may be written for two sequences.
+ */
+typedef struct a2ats_kv_blocks {
+  void* k;                    /* [dev, u8  piece * block * D]  codes                                    */
+  void* v;
+  float* k_scale;             /* [dev, f32 piece]                                                       */
+  float* v_scale;
+  void* k_tail;               /* [dev, kv_dtype B*Hkv*block*D] the tokens of each sequence's incomplete */
+  void* v_tail;               /*   block, token j in row j % block (never paged)                        */
+  void* bounds;               /* [dev, kv_dtype piece * 2 * D] smallest, then largest key per dimension */
+  const int32_t* page_table;
+  int32_t page_size;
+  int32_t block;
+  int32_t format;             /* A2ATS_I8 or A2ATS_E4M3                                                 */
+  int32_t kv_dtype;           /* of keys, values, queries, outputs, tails and bounds                    */
+} a2ats_kv_blocks;
+
+/*
+ * Append tokens to the cache.  Sequence b has seq_lens[b] (NULL: ctx_len) tokens afterwards; the last m_b of them are
+ * new, m_b = new_lens[b] [dev, nullable, int32 B] (NULL: n_new) limited to 0 .. min(n_new, seq_lens[b]): rows 0 .. m_b - 1 of
+ *   k_new, v_new [dev, kv_dtype B*Hkv*n_new*D]   pre-RoPE keys, and values
+ * A sequence only grows: the tokens before the new ones have been appended by earlier calls.  (It may begin again at 0.)
+ * A block is rounded when its last token is there, from the values as they were given (its earlier tokens come from the
+ * tail), so that the codes do not depend on how the tokens were cut into calls.  With a = max |x| over the block's
+ * block * D elements of keys (or of values) of a KV head:
+ *     A2ATS_I8    scale = fl32(a / 127), code = 127 x / a rounded to the nearest integer, ties to even (int8)
+ *     A2ATS_E4M3  scale = the least power of two with a <= 448 * scale, code = x / scale rounded to the nearest OCP e4m3 value,
+ *                 ties to even
+ * both as for real numbers; a code stands for code * scale.  a < 2^-100: scale 0 and codes 0.  A block with an element that
+ * is not finite: scale NaN and codes 0, so that what attends it is NaN.
+ * The tokens of an incomplete block are kept as they are in the tails (rows of tokens not there yet are not touched).
+ * bounds (if not NULL): for every block, complete or not, the smallest and largest key of its tokens per dimension, exactly
+ * (a NaN stays one).  Nothing else is written.  n_new == 0 is a no-op; n_new <= ctx_len.  One launch.
+ */
+int a2ats_kv8_append(const a2ats_dims* dims, const a2ats_kv_blocks* blocks, const void* k_new, const void* v_new,
+                     int32_t n_new, const int32_t* seq_lens, const int32_t* new_lens, void* stream);
+
+/*
+ * The bounds alone, for a caller whose cache is not in 8 bits: of `blocks` only bounds, block, kv_dtype, page_table and
+ * page_size are read.  Everything else as a2ats_kv8_append.
+ */
+int a2ats_key_bounds(const a2ats_dims* dims, const a2ats_kv_blocks* blocks, const void* k_new, int32_t n_new,
+                     const int32_t* seq_lens, const int32_t* new_lens, void* stream);
+
+/*
+ * Blocks selected by an upper bound of their tokens' logits.  Under WRoPE every token outside the window sees the query at one
+ * offset (section 4.1), q~ = q R_b, so that for the bounds lo, hi of a block's pre-RoPE keys
+ *     q~ . k_j  <=  score = sum_d max(q~_d lo_d, q~_d hi_d)    for every token j of the block.
+ * Candidates are the blocks that hold a candidate token, [sink_end, n - window) as in a2ats_score_topk; the top_blocks
+ * (<= 4096) with the highest scores are selected, equal scores to the lower block.  Scores are float64 sums rounded once to float32; a score that
+ * is not a number counts as infinite.
+ *   shared 0: for each query head, H = Hq;  otherwise: for each KV head, H = Hkv, score = the sum over its G query heads
+ *   q           [dev, kv_dtype B*Hq*D], cos_b / sin_b as in a2ats_build_lut, q_rot [dev, out, f32 B*Hq*D] as there (16-byte aligned)
+ *   block_idx   [dev, out, int32 B*H*top_blocks]  ascending, slots past block_count are -1
+ *   block_count [dev, out, int32 B*H]             min(top_blocks, candidates)
+ *   block_score [dev, out, nullable, f32 B*H*top_blocks]  (0 past block_count)
+ *   token_idx   [dev, out, nullable, int32 B*H*top_blocks*block] the candidate tokens of the selected blocks, ascending, then -1,
+ *   token_count [dev, out, nullable, int32 B*H]   and their number (both or neither): with
+ *               top_k = top_blocks * block these are the topk_idx / topk_count of a2ats_sparse_attn (shared:
+ *               a2ats_sparse_attn_shared) and its other forms.
+ * Of `blocks` only bounds, block, kv_dtype, page_table and page_size are read.
+ * Workspace: a2ats_workspace_bytes(dims, A2ATS_OP_BLOCK_TOPK, 0, 0).
+ */
+int a2ats_block_topk(const a2ats_dims* dims, const a2ats_kv_blocks* blocks, const void* q, const float* cos_b,
+                     const float* sin_b, float* q_rot, int32_t shared, int32_t top_blocks, int32_t window, int32_t n_sink,
+                     const int32_t* seq_lens, int32_t* block_idx, int32_t* block_count, float* block_score,
+                     int32_t* token_idx, int32_t* token_count, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * a2ats_sparse_attn over a cache in 8 bits that a2ats_kv8_append has brought to exactly seq_lens[b] (NULL: ctx_len) tokens a
+ * sequence.  The attended set is sinks U selection U window, where the selection of a head is
+ *   sel_idx   [dev, int32 B*H*n_sel], sel_count [dev, int32 B*H]   (n_sel <= 4096), in units of sel_size tokens:
+ *     sel_size 1: tokens, as a2ats_score_topk gives them;  sel_size == block: blocks, of which the candidate tokens are attended
+ *   shared 0: of each query head, H = Hq;  otherwise of each KV head, H = Hkv, attended by its G heads.
+ * Indices may be in any order but not repeat; what is not a candidate, [sink_end, n - window), is not attended.
+ * Rows of complete blocks are code * scale, those of the incomplete block are in the tails.  float32 accumulation; out
+ * [dev, out, kv_dtype B*Hq*D] is rounded once (zeros where nothing is attended).  q, q_rot, cos_win, sin_win as in
+ * a2ats_sparse_attn (all 16-byte aligned); `bounds` is not read.
+ * Workspace: a2ats_workspace_bytes(dims, A2ATS_OP_ATTN_KV8, n_sel * sel_size, window).
+ */
+int a2ats_sparse_attn_kv8(const a2ats_dims* dims, const a2ats_kv_blocks* blocks, const void* q, const float* q_rot,
+                          const int32_t* sel_idx, const int32_t* sel_count, int32_t n_sel, int32_t sel_size, int32_t shared,
+                          int32_t window, int32_t n_sink, const float* cos_win, const float* sin_win,
+                          const int32_t* seq_lens, void* out, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Offline codebook construction (paper section 4.2).

@@ -18,7 +18,8 @@ LIB_PATH = os.path.join(_HERE, "liba2ats.so")
 F32, BF16 = 0, 1
 W_NONE, W_DIAG, W_BLOCK = 0, 1, 2
 W_PREPARED = 0x100
-OP_ENCODE, OP_LUT, OP_SCORE_TOPK, OP_ATTN, OP_FIT, OP_SEED = 0, 1, 2, 3, 4, 5
+OP_ENCODE, OP_LUT, OP_SCORE_TOPK, OP_ATTN, OP_FIT, OP_SEED, OP_BLOCK_TOPK, OP_ATTN_KV8 = 0, 1, 2, 3, 4, 5, 6, 7
+I8, E4M3 = 0, 1
 EXPORTS = ["a2ats_version", "a2ats_status_string", "a2ats_lut_elems", "a2ats_workspace_bytes", "a2ats_encode_prepare",
            "a2ats_rope_tables", "a2ats_encode_keys", "a2ats_build_lut", "a2ats_score_topk",
            "a2ats_sparse_attn", "a2ats_score_topk_stats", "a2ats_score_topk_plan", "a2ats_score_topk_profiled",
@@ -26,7 +27,8 @@ EXPORTS = ["a2ats_version", "a2ats_status_string", "a2ats_lut_elems", "a2ats_wor
            "a2ats_decode_select_shared",
            "a2ats_second_moment", "a2ats_codebook_update", "a2ats_kmeanspp_seed", "a2ats_sparse_attn_paged",
            "a2ats_sparse_attn_static", "a2ats_score_topk_paged", "a2ats_codes_to_pages",
-           "a2ats_sparse_attn_host"]
+           "a2ats_sparse_attn_host", "a2ats_kv8_append", "a2ats_key_bounds", "a2ats_block_topk",
+           "a2ats_sparse_attn_kv8"]
 
 
 class A2atsError(RuntimeError):
@@ -39,6 +41,11 @@ class Dims(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("n_sub", ctypes.c_int32), ("sub_dim", ctypes.c_int32),
                 ("n_centroids", ctypes.c_int32), ("ctx_len", ctypes.c_int32), ("ctx_stride", ctypes.c_int64)]
+
+
+class KvBlocksStruct(ctypes.Structure):
+    _fields_ = [(x, ctypes.c_void_p) for x in ("k", "v", "k_scale", "v_scale", "k_tail", "v_tail", "bounds", "page_table")] + \
+               [(x, ctypes.c_int32) for x in ("page_size", "block", "format", "kv_dtype")]
 
 
 _lib = None
@@ -104,6 +111,15 @@ def lib() -> ctypes.CDLL:
         L.a2ats_score_topk_stats.argtypes = [dp, i32, i32, i32, vp, vp, vp]
         L.a2ats_score_topk_profiled.restype = ctypes.c_int
         L.a2ats_score_topk_profiled.argtypes = L.a2ats_score_topk.argtypes + [vp, vp]
+        bp = ctypes.POINTER(KvBlocksStruct)
+        L.a2ats_kv8_append.restype = ctypes.c_int
+        L.a2ats_kv8_append.argtypes = [dp, bp, vp, vp, i32, vp, vp, vp]
+        L.a2ats_key_bounds.restype = ctypes.c_int
+        L.a2ats_key_bounds.argtypes = [dp, bp, vp, i32, vp, vp, vp]
+        L.a2ats_block_topk.restype = ctypes.c_int
+        L.a2ats_block_topk.argtypes = [dp, bp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.a2ats_sparse_attn_kv8.restype = ctypes.c_int
+        L.a2ats_sparse_attn_kv8.argtypes = [dp, bp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -346,6 +362,182 @@ def codes_to_pages(dims: Dims, new_codes, n_new: int, pos0: int, code_pool, page
     _check(rc, "a2ats_codes_to_pages")
 
 
+class KvBlocks:
+    """A key/value cache cut into blocks of tokens (a2ats_kv_blocks): the tensors and their description, nothing else.
+
+    k, v           int8 or float8_e4m3fn, [B, Hkv, ctx_stride, D], or pages [pages, Hkv, page_size, D]
+    k_scale, ...   float32 [.., ctx_stride / block] (pages: page_size / block)
+    k_tail, ...    kv_dtype [B, Hkv, block, D]
+    bounds         kv_dtype [.., ctx_stride / block, 2, D] (pages: page_size / block)
+    All of k .. v_tail are None for a cache of which only the bounds are kept here (key_bounds, block_topk)."""
+
+    def __init__(self, dims: Dims, block: int, kv_dtype: torch.dtype, k=None, v=None, k_scale=None, v_scale=None, k_tail=None,
+                 v_tail=None, bounds=None, page_table=None, page_size: int = 0):
+        rows = (k, v, k_scale, v_scale, k_tail, v_tail)
+        if any(t is None for t in rows) != all(t is None for t in rows):
+            raise ValueError("k, v, their scales and tails are given together")
+        if k is None and bounds is None:
+            raise ValueError("neither rows nor bounds")
+        if kv_dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"unsupported dtype {kv_dtype}")
+        if block not in (16, 32, 64, 128):
+            raise ValueError("block is 16, 32, 64 or 128")
+        B, Hkv, D = dims.batch, dims.n_kv_heads, dims.head_dim
+        if page_table is not None:
+            if page_size < block or page_size & (page_size - 1):
+                raise ValueError("page_size is a power of two of at least a block")
+            some = k if k is not None else bounds
+            lead = (some.shape[0], Hkv)
+            slots = page_size
+            _check_tensor(page_table, "page_table", torch.int32, (B, -(-dims.ctx_stride // page_size)))
+        else:
+            if dims.ctx_stride % block:
+                raise ValueError("ctx_stride is a multiple of block")
+            lead, slots = (B, Hkv), int(dims.ctx_stride)
+        self.format = I8
+        if k is not None:
+            if k.dtype not in (torch.int8, torch.float8_e4m3fn):
+                raise TypeError(f"codes are int8 or float8_e4m3fn, not {k.dtype}")
+            self.format = I8 if k.dtype == torch.int8 else E4M3
+            for name, t in (("k", k), ("v", v)):
+                _check_tensor(t, name, k.dtype, lead + (slots, D))
+            for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+                _check_tensor(t, name, torch.float32, lead + (slots // block,))
+            for name, t in (("k_tail", k_tail), ("v_tail", v_tail)):
+                _check_tensor(t, name, kv_dtype, (B, Hkv, block, D))
+        if bounds is not None:
+            _check_tensor(bounds, "bounds", kv_dtype, lead + (slots // block, 2, D))
+        self.block, self.kv_dtype, self.page_size, self.page_table = block, kv_dtype, page_size, page_table
+        self.k, self.v, self.k_scale, self.v_scale, self.k_tail, self.v_tail, self.bounds = k, v, k_scale, v_scale, k_tail, v_tail, bounds
+        self.device = (k if k is not None else bounds).device
+        for t in rows + (bounds, page_table):
+            if t is not None and t.device != self.device:
+                raise ValueError("the tensors of a cache are on one device")
+        p = [None if t is None else t.data_ptr() for t in (k, v, k_scale, v_scale, k_tail, v_tail, bounds, page_table)]
+        self.struct = KvBlocksStruct(*p, page_size, block, self.format, F32 if kv_dtype == torch.float32 else BF16)
+        self.ref = ctypes.byref(self.struct)
+        self.batch, self.n_kv_heads, self.ctx_stride = B, Hkv, int(dims.ctx_stride)
+
+    @classmethod
+    def empty(cls, dims: Dims, block: int, kv_dtype: torch.dtype, codes: Optional[torch.dtype] = torch.int8, bounds: bool = True,
+              page_table=None, page_size: int = 0, n_pages: int = 0, device="cuda"):
+        """A cache in new memory (scales zero).  codes None: only the bounds."""
+        B, Hkv, D = dims.batch, dims.n_kv_heads, dims.head_dim
+        lead, slots = ((n_pages, Hkv), page_size) if page_table is not None else ((B, Hkv), int(dims.ctx_stride))
+        t = {}
+        if codes is not None:
+            for x in ("k", "v"):
+                t[x] = torch.empty(lead + (slots, D), dtype=codes, device=device)
+                t[x + "_scale"] = torch.zeros(lead + (slots // block,), dtype=torch.float32, device=device)
+                t[x + "_tail"] = torch.zeros(B, Hkv, block, D, dtype=kv_dtype, device=device)
+        if bounds:
+            t["bounds"] = torch.empty(lead + (slots // block, 2, D), dtype=kv_dtype, device=device)
+        return cls(dims, block, kv_dtype, page_table=page_table, page_size=page_size, **t)
+
+
+def _check_tensor(t: torch.Tensor, name: str, dtype: torch.dtype, shape):
+    if t.dtype != dtype:
+        raise TypeError(f"{name} is {t.dtype}, not {dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} is not contiguous")
+
+
+def _arg(cache: KvBlocks, t: Optional[torch.Tensor], name: str, dtype: torch.dtype, numel: int):
+    """Pointer of a tensor of a call on `cache`: of its device, its type and `numel` elements."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError(f"{name} is {t.dtype}, not {dtype}")
+    if t.device != cache.device:
+        raise ValueError(f"{name} is on {t.device}, the cache on {cache.device}")
+    if t.numel() != numel or not t.is_contiguous():
+        raise ValueError(f"{name}: {numel} contiguous elements are wanted, not {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _cache_stream(dims: Dims, cache: KvBlocks):
+    if (dims.batch, dims.n_kv_heads, dims.ctx_stride) != (cache.batch, cache.n_kv_heads, cache.ctx_stride):
+        raise ValueError("dims are not those of the cache")
+    if cache.device.type != "cuda":
+        raise ValueError(f"the cache is on {cache.device}")
+    if cache.device.index != torch.cuda.current_device():
+        raise ValueError(f"the cache is on {cache.device}, the current device is {torch.cuda.current_device()}")
+    return torch.cuda.current_stream().cuda_stream
+
+
+def kv8_append(dims: Dims, cache: KvBlocks, k_new, v_new, n_new: int, seq_lens=None, new_lens=None):
+    """Append up to n_new tokens a sequence, k_new / v_new [B, Hkv, n_new, D]; seq_lens count them already."""
+    B, n = dims.batch, dims.batch * dims.n_kv_heads * n_new * dims.head_dim
+    st = _cache_stream(dims, cache)
+    rc = lib().a2ats_kv8_append(ctypes.byref(dims), cache.ref, _arg(cache, k_new, "k_new", cache.kv_dtype, n),
+                                _arg(cache, v_new, "v_new", cache.kv_dtype, n), n_new,
+                                _arg(cache, seq_lens, "seq_lens", torch.int32, B),
+                                _arg(cache, new_lens, "new_lens", torch.int32, B), st)
+    _check(rc, "a2ats_kv8_append")
+
+
+def key_bounds(dims: Dims, cache: KvBlocks, k_new, n_new: int, seq_lens=None, new_lens=None):
+    """The bounds of the appended tokens' blocks alone."""
+    st = _cache_stream(dims, cache)
+    rc = lib().a2ats_key_bounds(ctypes.byref(dims), cache.ref,
+                                _arg(cache, k_new, "k_new", cache.kv_dtype, dims.batch * dims.n_kv_heads * n_new * dims.head_dim),
+                                n_new, _arg(cache, seq_lens, "seq_lens", torch.int32, dims.batch),
+                                _arg(cache, new_lens, "new_lens", torch.int32, dims.batch), st)
+    _check(rc, "a2ats_key_bounds")
+
+
+def block_topk(dims: Dims, cache: KvBlocks, q, cos_b, sin_b, q_rot, shared: bool, top_blocks: int, window: int, n_sink: int,
+               seq_lens, block_idx, block_count, block_score=None, token_idx=None, token_count=None,
+               ws: Optional[torch.Tensor] = None):
+    """Rotate the query and select the top_blocks blocks of each query head (shared: of each KV head)."""
+    n_q = dims.batch * dims.n_q_heads * dims.head_dim
+    n_h = dims.batch * (dims.n_kv_heads if shared else dims.n_q_heads)
+    half = dims.head_dim // 2
+    st = _cache_stream(dims, cache)
+    rc = lib().a2ats_block_topk(ctypes.byref(dims), cache.ref, _arg(cache, q, "q", cache.kv_dtype, n_q),
+                                _arg(cache, cos_b, "cos_b", torch.float32, half), _arg(cache, sin_b, "sin_b", torch.float32, half),
+                                _arg(cache, q_rot, "q_rot", torch.float32, n_q), int(shared), top_blocks, window, n_sink,
+                                _arg(cache, seq_lens, "seq_lens", torch.int32, dims.batch),
+                                _arg(cache, block_idx, "block_idx", torch.int32, n_h * top_blocks),
+                                _arg(cache, block_count, "block_count", torch.int32, n_h),
+                                _arg(cache, block_score, "block_score", torch.float32, n_h * top_blocks),
+                                _arg(cache, token_idx, "token_idx", torch.int32, n_h * top_blocks * cache.block),
+                                _arg(cache, token_count, "token_count", torch.int32, n_h), _ws_ptr(cache, ws), _ws_bytes(ws), st)
+    _check(rc, "a2ats_block_topk")
+
+
+def sparse_attn_kv8(dims: Dims, cache: KvBlocks, q, q_rot, sel_idx, sel_count, n_sel: int, sel_size: int, shared: bool,
+                    window: int, n_sink: int, cos_win, sin_win, seq_lens, out, ws: Optional[torch.Tensor] = None):
+    """Attention over sinks, selection (tokens: sel_size 1, or blocks: sel_size cache.block) and window of an 8-bit cache."""
+    n_q = dims.batch * dims.n_q_heads * dims.head_dim
+    n_h = dims.batch * (dims.n_kv_heads if shared else dims.n_q_heads)
+    n_w = max(window, 1) * (dims.head_dim // 2)
+    st = _cache_stream(dims, cache)
+    rc = lib().a2ats_sparse_attn_kv8(ctypes.byref(dims), cache.ref, _arg(cache, q, "q", cache.kv_dtype, n_q),
+                                     _arg(cache, q_rot, "q_rot", torch.float32, n_q),
+                                     _arg(cache, sel_idx, "sel_idx", torch.int32, n_h * n_sel),
+                                     _arg(cache, sel_count, "sel_count", torch.int32, n_h), n_sel, sel_size, int(shared), window,
+                                     n_sink, _arg(cache, cos_win, "cos_win", torch.float32, n_w),
+                                     _arg(cache, sin_win, "sin_win", torch.float32, n_w),
+                                     _arg(cache, seq_lens, "seq_lens", torch.int32, dims.batch),
+                                     _arg(cache, out, "out", cache.kv_dtype, n_q), _ws_ptr(cache, ws), _ws_bytes(ws), st)
+    _check(rc, "a2ats_sparse_attn_kv8")
+
+
+def _ws_ptr(cache: KvBlocks, ws: Optional[torch.Tensor]):
+    if ws is None:
+        return None
+    if ws.device != cache.device or not ws.is_contiguous():
+        raise ValueError("the workspace is contiguous and on the cache's device")
+    return ws.data_ptr()
+
+
+def _ws_bytes(ws: Optional[torch.Tensor]) -> int:
+    return 0 if ws is None else ws.numel() * ws.element_size()
+
+
 PLAN_FIELDS = ("fast", "head_groups", "sample_parts", "sample_rows", "chunks", "rows_per_chunk",
                "segments_per_wave", "rows_per_segment", "segment_capacity", "survivor_capacity",
                "workspace_bytes_div_256")
@@ -406,4 +598,31 @@ class DecodeState:
                    self.scores if with_scores else None, self.ws)
         sparse_attn(self.dims, q, self.q_rot, k_cache, v_cache, self.topk_idx, self.topk_count, self.top_k,
                     self.window, self.n_sink, self.cos_win, self.sin_win, seq_lens, self.out, self.ws)
+        return self.out
+
+
+class BlockDecodeState:
+    """Device buffers for decode steps over a KvBlocks cache (allocation only; no arithmetic)."""
+
+    def __init__(self, dims: Dims, cache: KvBlocks, top_blocks: int, window: int, n_sink: int, inv_freq: torch.Tensor,
+                 wrope_b: int, shared: bool = False):
+        self.dims, self.cache, self.top_blocks, self.window, self.n_sink, self.shared = dims, cache, top_blocks, window, n_sink, shared
+        B, Hq, D, dev = dims.batch, dims.n_q_heads, dims.head_dim, cache.device
+        heads = dims.n_kv_heads if shared else Hq
+        self.cos_b, self.sin_b, self.cos_win, self.sin_win = rope_tables(D, inv_freq, wrope_b, window, dev)
+        self.q_rot = torch.empty(B, Hq, D, dtype=torch.float32, device=dev)
+        self.block_idx = torch.empty(B, heads, top_blocks, dtype=torch.int32, device=dev)
+        self.block_count = torch.empty(B, heads, dtype=torch.int32, device=dev)
+        self.block_score = torch.empty(B, heads, top_blocks, dtype=torch.float32, device=dev)
+        self.out = torch.empty(B, Hq, D, dtype=cache.kv_dtype, device=dev)
+        n_ws = max(workspace_bytes(dims, OP_BLOCK_TOPK), workspace_bytes(dims, OP_ATTN_KV8, top_blocks * cache.block, window), 256)
+        self.ws = torch.empty(n_ws, dtype=torch.uint8, device=dev)
+
+    def step(self, q, k_new, v_new, seq_lens=None):
+        """kv8_append of one token a sequence -> block_topk -> sparse_attn_kv8 on the current stream; returns self.out."""
+        kv8_append(self.dims, self.cache, k_new, v_new, 1, seq_lens)
+        block_topk(self.dims, self.cache, q, self.cos_b, self.sin_b, self.q_rot, self.shared, self.top_blocks, self.window,
+                   self.n_sink, seq_lens, self.block_idx, self.block_count, self.block_score, ws=self.ws)
+        sparse_attn_kv8(self.dims, self.cache, q, self.q_rot, self.block_idx, self.block_count, self.top_blocks, self.cache.block,
+                        self.shared, self.window, self.n_sink, self.cos_win, self.sin_win, seq_lens, self.out, self.ws)
         return self.out

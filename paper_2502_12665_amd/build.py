@@ -10,7 +10,8 @@ _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "liba2ats.so")
 SOURCES = ["a2ats_api.hip", "build_lut.hip", "score_topk.hip", "sparse_attn.hip", "encode_keys.hip",
-           "single_codebook.hip", "encode_single.hip", "codebook_fit.hip"]
+           "single_codebook.hip", "encode_single.hip", "codebook_fit.hip", "kv8_append.hip", "block_topk.hip",
+           "sparse_attn_kv8.hip"]
 HOST_SOURCES = ["attn_host.cpp"]   # host-only code (OpenMP + SIMD): the CPU side of the heterogeneous placement
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",

@@ -48,6 +48,46 @@ int check_dims(const a2ats_dims* d) {
 
 bool misaligned16(const void* p) { return ((uintptr_t)p & 15u) != 0; }
 
+// The blocks of a cache: what the kernels are given, and whether they can be.
+constexpr int kLeastBlock = 16, kLargestBlock = 128;
+int log2_of(int v) {
+  int s = 0;
+  while ((1 << s) < v) ++s;
+  return s;
+}
+int check_blocks(const a2ats_dims& d, const a2ats_kv_blocks* c, bool rows, bool bounds, a2ats::BlockCache* m) {
+  if (!c) return A2ATS_ERR_INVALID_ARG;
+  if (c->block < kLeastBlock || (c->block & (c->block - 1))) return A2ATS_ERR_INVALID_ARG;
+  if (c->block > kLargestBlock) return A2ATS_ERR_UNSUPPORTED;
+  if (c->kv_dtype != A2ATS_F32 && c->kv_dtype != A2ATS_BF16) return A2ATS_ERR_INVALID_ARG;
+  if (rows) {
+    if (c->format != A2ATS_I8 && c->format != A2ATS_E4M3) return A2ATS_ERR_INVALID_ARG;
+    if (!c->k || !c->v || !c->k_scale || !c->v_scale || !c->k_tail || !c->v_tail) return A2ATS_ERR_INVALID_ARG;
+    if (misaligned16(c->k) || misaligned16(c->v) || misaligned16(c->k_tail) || misaligned16(c->v_tail)) return A2ATS_ERR_INVALID_ARG;
+  }
+  if ((bounds && !c->bounds) || misaligned16(c->bounds)) return A2ATS_ERR_INVALID_ARG;
+  *m = {};
+  m->k = (uint8_t*)c->k;
+  m->v = (uint8_t*)c->v;
+  m->k_scale = c->k_scale;
+  m->v_scale = c->v_scale;
+  m->k_tail = c->k_tail;
+  m->v_tail = c->v_tail;
+  m->bounds = c->bounds;
+  m->shift = log2_of(c->block);
+  m->n_kv_heads = d.n_kv_heads;
+  if (c->page_table) {
+    if (c->page_size < c->block || (c->page_size & (c->page_size - 1))) return A2ATS_ERR_INVALID_ARG;
+    m->pages = c->page_table;
+    m->page_shift = log2_of(c->page_size) - m->shift;
+    m->pages_per_seq = (int32_t)((d.ctx_stride + c->page_size - 1) / c->page_size);
+  } else {
+    if (d.ctx_stride % c->block) return A2ATS_ERR_INVALID_ARG;
+    m->blocks_per_seq = d.ctx_stride / c->block;
+  }
+  return A2ATS_OK;
+}
+
 // Whether `ws` can hold a selection plan's workspace.  The streaming route refuses to run without; a
 // wide plan then takes the exact route instead, which needs none (selections of more than 2048 tokens
 // used to ask for no workspace at all).
@@ -113,6 +153,16 @@ size_t a2ats_workspace_bytes(const a2ats_dims* d, int op, int32_t top_k, int32_t
       // The number of workgroups per head grows with the attended rows; sized for up to 64 sinks
       // (a call with more sinks than that may ask for more and is refused if `ws` is too small).
       return a2ats::make_attn_plan(*d, top_k, window, 64).bytes;
+    }
+    case A2ATS_OP_BLOCK_TOPK: {   // of the smallest blocks, a selection per head
+      if (top_k < 0 || window < 0) return (size_t)-1;
+      return a2ats::make_block_topk_plan(*d, kLeastBlock, false).bytes;
+    }
+    case A2ATS_OP_ATTN_KV8: {   // the larger of the two kinds of selection
+      if (top_k < 0 || window < 0) return (size_t)-1;
+      const size_t own = a2ats::make_kv8_plan(*d, top_k, window, false).bytes;
+      const size_t shared = a2ats::make_kv8_plan(*d, top_k, window, true).bytes;
+      return own > shared ? own : shared;
     }
     case A2ATS_OP_FIT: return a2ats::fit_ws_bytes(*d);
     case A2ATS_OP_SEED: return a2ats::single_codebook(*d) ? a2ats::kmeanspp_ws_bytes(*d) : (size_t)-1;
@@ -629,6 +679,78 @@ int a2ats_sparse_attn_shared(const a2ats_dims* d, const void* q, const float* q_
                              void* ws, size_t ws_bytes, void* stream) {
   return sparse_attn_impl(d, q, q_rot, k_cache, v_cache, kv_dtype, topk_idx, topk_count, top_k, window, n_sink,
                           cos_win, sin_win, seq_lens, out, ws, ws_bytes, true, nullptr, 0, stream);
+}
+
+static int append_impl(const a2ats_dims* d, const a2ats_kv_blocks* blocks, bool rows, const void* k_new, const void* v_new,
+                       int32_t n_new, const int32_t* seq_lens, const int32_t* new_lens, void* stream) {
+  int rc = check_dims(d);
+  if (rc != A2ATS_OK) return rc;
+  a2ats::BlockCache m;
+  rc = check_blocks(*d, blocks, rows, !rows, &m);
+  if (rc != A2ATS_OK) return rc;
+  if (n_new < 0 || n_new > d->ctx_len) return A2ATS_ERR_INVALID_ARG;
+  if (!k_new || misaligned16(k_new) || (rows && (!v_new || misaligned16(v_new)))) return A2ATS_ERR_INVALID_ARG;
+  if ((int64_t)d->batch * d->n_kv_heads * a2ats::append_parts(n_new, blocks->block) * 2 >= (1LL << 31)) return A2ATS_ERR_UNSUPPORTED;
+  const hipError_t e = a2ats::launch_append(*d, m, blocks->kv_dtype, blocks->format, rows, k_new, v_new, n_new, seq_lens,
+                                            new_lens, (hipStream_t)stream);
+  return e == hipSuccess ? A2ATS_OK : A2ATS_ERR_HIP;
+}
+
+int a2ats_kv8_append(const a2ats_dims* d, const a2ats_kv_blocks* blocks, const void* k_new, const void* v_new, int32_t n_new,
+                     const int32_t* seq_lens, const int32_t* new_lens, void* stream) {
+  return append_impl(d, blocks, true, k_new, v_new, n_new, seq_lens, new_lens, stream);
+}
+
+int a2ats_key_bounds(const a2ats_dims* d, const a2ats_kv_blocks* blocks, const void* k_new, int32_t n_new,
+                     const int32_t* seq_lens, const int32_t* new_lens, void* stream) {
+  return append_impl(d, blocks, false, k_new, nullptr, n_new, seq_lens, new_lens, stream);
+}
+
+int a2ats_block_topk(const a2ats_dims* d, const a2ats_kv_blocks* blocks, const void* q, const float* cos_b, const float* sin_b,
+                     float* q_rot, int32_t shared, int32_t top_blocks, int32_t window, int32_t n_sink, const int32_t* seq_lens,
+                     int32_t* block_idx, int32_t* block_count, float* block_score, int32_t* token_idx, int32_t* token_count,
+                     void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_dims(d);
+  if (rc != A2ATS_OK) return rc;
+  a2ats::BlockCache m;
+  rc = check_blocks(*d, blocks, false, true, &m);
+  if (rc != A2ATS_OK) return rc;
+  if (top_blocks < 0 || window < 0 || n_sink < 0) return A2ATS_ERR_INVALID_ARG;
+  if (top_blocks > 4096) return A2ATS_ERR_UNSUPPORTED;
+  if (!q || !cos_b || !sin_b || !q_rot || !block_count || (top_blocks > 0 && !block_idx)) return A2ATS_ERR_INVALID_ARG;
+  if ((token_idx == nullptr) != (token_count == nullptr)) return A2ATS_ERR_INVALID_ARG;
+  if (misaligned16(q) || misaligned16(cos_b) || misaligned16(sin_b) || misaligned16(q_rot)) return A2ATS_ERR_INVALID_ARG;
+  const a2ats::BlockTopkPlan plan = a2ats::make_block_topk_plan(*d, blocks->block, shared != 0);
+  if ((int64_t)d->batch * d->n_kv_heads * plan.chunks >= (1LL << 31)) return A2ATS_ERR_UNSUPPORTED;
+  if (plan.bytes > 0 && (!ws || misaligned16(ws) || ws_bytes < plan.bytes)) return A2ATS_ERR_WORKSPACE;
+  const hipError_t e = a2ats::launch_block_topk(*d, m, blocks->kv_dtype, q, cos_b, sin_b, q_rot, shared != 0, top_blocks, window,
+                                                n_sink, seq_lens, block_idx, block_count, block_score, token_idx, token_count,
+                                                ws, (hipStream_t)stream);
+  return e == hipSuccess ? A2ATS_OK : A2ATS_ERR_HIP;
+}
+
+int a2ats_sparse_attn_kv8(const a2ats_dims* d, const a2ats_kv_blocks* blocks, const void* q, const float* q_rot,
+                          const int32_t* sel_idx, const int32_t* sel_count, int32_t n_sel, int32_t sel_size, int32_t shared,
+                          int32_t window, int32_t n_sink, const float* cos_win, const float* sin_win, const int32_t* seq_lens,
+                          void* out, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_dims(d);
+  if (rc != A2ATS_OK) return rc;
+  a2ats::BlockCache m;
+  rc = check_blocks(*d, blocks, true, false, &m);
+  if (rc != A2ATS_OK) return rc;
+  if (n_sel < 0 || window < 0 || n_sink < 0) return A2ATS_ERR_INVALID_ARG;
+  if (sel_size != 1 && sel_size != blocks->block) return A2ATS_ERR_INVALID_ARG;
+  if (n_sel > 4096) return A2ATS_ERR_UNSUPPORTED;
+  if (!q || !q_rot || !sel_count || !out || (n_sel > 0 && !sel_idx)) return A2ATS_ERR_INVALID_ARG;
+  if (window > 0 && (!cos_win || !sin_win)) return A2ATS_ERR_INVALID_ARG;
+  if (misaligned16(q) || misaligned16(q_rot) || misaligned16(cos_win) || misaligned16(sin_win)) return A2ATS_ERR_INVALID_ARG;
+  const a2ats::Kv8Plan plan = a2ats::make_kv8_plan(*d, (long)n_sel * sel_size, window, shared != 0);
+  if ((int64_t)d->batch * d->n_q_heads * plan.parts >= (1LL << 31)) return A2ATS_ERR_UNSUPPORTED;
+  if (plan.bytes > 0 && (!ws || misaligned16(ws) || ws_bytes < plan.bytes)) return A2ATS_ERR_WORKSPACE;
+  const hipError_t e = a2ats::launch_sparse_attn_kv8(*d, m, blocks->kv_dtype, blocks->format, q, q_rot, sel_idx, sel_count, n_sel,
+                                                     log2_of(sel_size), shared != 0, window, n_sink, cos_win, sin_win, seq_lens,
+                                                     out, ws, (hipStream_t)stream);
+  return e == hipSuccess ? A2ATS_OK : A2ATS_ERR_HIP;
 }
 
 int a2ats_score_topk_stats(const a2ats_dims* d, int32_t top_k, int32_t window, int32_t n_sink, const void* ws,

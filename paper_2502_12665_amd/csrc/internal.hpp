@@ -10,6 +10,7 @@
 
 #include "a2ats.h"
 #include "common.hpp"
+#include "kv_blocks.hpp"
 
 namespace a2ats {
 
@@ -190,6 +191,30 @@ hipError_t launch_second_moment(const a2ats_dims& d, const float* q_rot, int64_t
 hipError_t launch_codebook_update(const a2ats_dims& d, const float* keys, int n_new, int pos0, const void* codes,
                                   const float* codebook, float* codebook_out, int32_t* counts_out, void* ws,
                                   size_t ws_bytes, hipStream_t stream);
+
+// A cache cut into blocks (kv_blocks.hpp): append (codes: the 8-bit rows too, else the bounds alone), selection, attention.
+int append_parts(int n_new, int block);   // workgroups of a sequence and KV head's keys
+hipError_t launch_append(const a2ats_dims& d, const BlockCache& m, int kv_dtype, int format, bool codes, const void* k_new,
+                         const void* v_new, int n_new, const int32_t* seq_lens, const int32_t* new_lens, hipStream_t stream);
+struct BlockTopkPlan {
+  int total_blocks;     // of ctx_len tokens
+  int chunk, chunks;    // blocks that a scoring workgroup takes, and workgroups of a (sequence, KV head)
+  size_t bytes;         // the scores
+};
+BlockTopkPlan make_block_topk_plan(const a2ats_dims& d, int block, bool shared);
+hipError_t launch_block_topk(const a2ats_dims& d, const BlockCache& m, int kv_dtype, const void* q, const float* cos_b,
+                             const float* sin_b, float* q_rot, bool shared, int top_blocks, int window, int n_sink,
+                             const int32_t* seq_lens, int32_t* block_idx, int32_t* block_count, float* block_score,
+                             int32_t* token_idx, int32_t* token_count, void* ws, hipStream_t stream);
+struct Kv8Plan {
+  int parts;            // workgroups among which a head's rows (shared selection: a KV head's) are shared out; not by the sinks
+  size_t bytes;         // their states; 0 if there is one
+};
+Kv8Plan make_kv8_plan(const a2ats_dims& d, long sel_rows, int window, bool shared);
+hipError_t launch_sparse_attn_kv8(const a2ats_dims& d, const BlockCache& m, int kv_dtype, int format, const void* q,
+                                  const float* q_rot, const int32_t* sel_idx, const int32_t* sel_count, int n_sel, int sel_shift,
+                                  bool shared, int window, int n_sink, const float* cos_win, const float* sin_win,
+                                  const int32_t* seq_lens, void* out, void* ws, hipStream_t stream);
 
 // Copy freshly encoded code rows [B][Hkv][n_new][row_bytes] to tokens pos0 .. pos0 + n_new - 1 of a paged pool.
 hipError_t launch_codes_to_pages(const a2ats_dims& d, const uint8_t* rows, int n_new, int pos0, int row_bytes,

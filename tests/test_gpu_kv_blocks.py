@@ -1,0 +1,637 @@
+"""The operators on a cache cut into blocks (a2ats_kv8_append, a2ats_key_bounds, a2ats_block_topk, a2ats_sparse_attn_kv8)
+against plain float64 forms, through the C ABI."""
+import math
+
+import pytest
+import torch
+
+from paper_2502_12665_amd import binding as B
+from paper_2502_12665_amd import synth
+from tests import kv_blocks_ref as R
+
+pytestmark = pytest.mark.gpu
+D = 128
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+CODES = {"i8": torch.int8, "e4m3": torch.float8_e4m3fn}
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def dims_of(batch, heads, kv_heads, ctx, stride):
+    return B.make_dims(batch, heads, kv_heads, D, 16, ctx, stride)
+
+
+def up(n, m):
+    return max(m, -(-n // m) * m)
+
+
+class Case:
+    """Sequences in host memory, and a cache on the GPU that appends fill."""
+
+    def __init__(self, lens, heads, kv_heads, blk, fmt, dtype, page=0, seed=0, bounds=True, spread=1.0, ctx=None):
+        self.lens, self.blk, self.fmt, self.dtype, self.page = list(lens), blk, fmt, DT[dtype], page
+        self.heads, self.kv_heads, self.G = heads, kv_heads, heads // kv_heads
+        self.batch, self.ctx = len(lens), max(max(lens), 1) if ctx is None else ctx
+        self.stride = up(self.ctx, page or blk)
+        g = gen(seed)
+        self.k = [(spread * torch.randn(kv_heads, n, D, generator=g)).to(self.dtype) for n in lens]
+        self.v = [torch.randn(kv_heads, n, D, generator=g).to(self.dtype) for n in lens]
+        self.q = torch.randn(self.batch, heads, D, generator=g).to(self.dtype)
+        self.dims = dims_of(self.batch, heads, kv_heads, self.ctx, self.stride)
+        table, n_pages = None, 0
+        if page:
+            slots = self.stride // page
+            n_pages = self.batch * slots + 3
+            table = torch.randperm(n_pages, generator=g)[: self.batch * slots].reshape(self.batch, slots).int().cuda()
+        self.cache = B.KvBlocks.empty(self.dims, blk, self.dtype, CODES[fmt], bounds, table, page, n_pages)
+        for t in (self.cache.k, self.cache.v):
+            t.view(torch.uint8).fill_(0x2A)
+        for t in (self.cache.k_scale, self.cache.v_scale, self.cache.k_tail, self.cache.v_tail) + ((self.cache.bounds,) if bounds else ()):
+            t.fill_(-77.0)
+        self.inv = synth.inv_freq(D, 500000.0)
+        self.have = [0] * self.batch
+
+    def append(self, upto, use_lens=True, n_new=None, stream=None):
+        """Bring sequence b to upto[b] tokens by one call."""
+        m = [u - h for u, h in zip(upto, self.have)]
+        n_new = max(max(m), 1) if n_new is None else n_new
+        new = {x: torch.full((self.batch, self.kv_heads, n_new, D), 5.0, dtype=self.dtype) for x in "kv"}
+        for b, (h, u) in enumerate(zip(self.have, upto)):
+            new["k"][b, :, : u - h] = self.k[b][:, h:u]
+            new["v"][b, :, : u - h] = self.v[b][:, h:u]
+        lens = torch.tensor(upto, dtype=torch.int32, device="cuda")
+        news = torch.tensor(m, dtype=torch.int32, device="cuda") if use_lens else None
+        B.kv8_append(self.dims, self.cache, new["k"].cuda(), new["v"].cuda(), n_new, lens, news)
+        self.have = list(upto)
+
+    def piece(self, t, b, kv):
+        """Part of a cache tensor that belongs to (b, kv): [slots, ...], pages put behind each other."""
+        t = t.cpu()
+        if not self.page:
+            return t[b, kv]
+        return torch.cat([t[p, kv] for p in self.cache.page_table[b].tolist()])
+
+    def seq(self, b, kv, n=None):
+        n = self.lens[b] if n is None else n
+        return R.Sequence(self.k[b][kv, :n], self.v[b][kv, :n], self.blk, self.fmt)
+
+    def check_cache(self):
+        """Everything that the cache holds is what the sequences so far say, and the rest is untouched."""
+        torch.cuda.synchronize()
+        for b in range(self.batch):
+            n = self.have[b]
+            full, touched = n // self.blk, -(-n // self.blk)
+            for kv in range(self.kv_heads):
+                want = self.seq(b, kv, n)
+                for x in "kv":
+                    raw = self.piece(getattr(self.cache, x), b, kv)
+                    got = raw.float().double().reshape(-1, self.blk, D)
+                    assert torch.equal(got[:full], want.codes[x]), (b, kv, x)
+                    assert (raw.view(torch.uint8).reshape(-1, self.blk, D)[full:] == 0x2A).all(), (b, kv, x)
+                    sc = self.piece(getattr(self.cache, x + "_scale"), b, kv).double()
+                    assert torch.equal(torch.nan_to_num(sc[:full], nan=-1.0), torch.nan_to_num(want.scales[x], nan=-1.0))
+                    assert (sc[full:] == -77).all()
+                    tail = getattr(self.cache, x + "_tail")[b, kv].cpu()
+                    rest = getattr(self, x)[b][kv, full * self.blk:n]
+                    assert torch.equal(tail[: n - full * self.blk], rest)
+                if self.cache.bounds is not None:
+                    bd = self.piece(self.cache.bounds, b, kv).double()
+                    assert torch.equal(bd[:touched], want.bounds), (b, kv)
+                    assert (bd[touched:] == -77).all()
+
+
+# ---------------------------------------------------------------------------------------------- append
+
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("blk, page", [(16, 0), (32, 64), (64, 64), (128, 0), (128, 256)])
+def test_append_in_pieces(fmt, dtype, blk, page):
+    """One token, a few, across block borders, more than a workgroup's 128 rows, different numbers a sequence: after every
+    call codes, scales, tails and bounds are those of the whole sequences, and nothing else was written."""
+    c = Case([400, 37, 1, 0, 261], 4, 2, blk, fmt, dtype, page, seed=blk + page)
+    steps = [[1, 0, 0, 0, 5], [2, 1, 1, 0, 5], [blk - 1, 16, 1, 0, 6], [blk, 17, 1, 0, blk + 1], [blk + 1, 17, 1, 0, blk + 1],
+             [min(400, blk + 130), 36, 1, 0, 200], [400, 37, 1, 0, 261]]
+    for s in steps:
+        c.append(s)
+        c.check_cache()
+
+
+def test_append_all_at_once_and_padded():
+    """Prefill of prompts of different lengths in one padded call: without new_lens a sequence's tokens are its first rows."""
+    c = Case([300, 1, 64, 0, 129], 7, 1, 32, "i8", "bf16", seed=3)
+    c.append(c.lens, use_lens=False, n_new=300)
+    c.check_cache()
+    one = Case([515, 515], 8, 8, 64, "e4m3", "f32", seed=4, bounds=False)
+    one.append([515, 515], use_lens=False)
+    one.check_cache()
+
+
+def test_append_without_lengths():
+    """seq_lens NULL: every sequence has ctx_len tokens."""
+    c = Case([70, 70], 2, 2, 16, "i8", "bf16", seed=5)
+    new = [torch.stack(t).cuda() for t in (c.k, c.v)]
+    B.kv8_append(c.dims, c.cache, new[0], new[1], 70)
+    c.have = [70, 70]
+    c.check_cache()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rounding_of_ties(dtype):
+    """127 x / a on and next to halves: ties to even, and the numbers beside them to their own side."""
+    c = Case([16], 1, 1, 16, "i8", dtype, seed=6)
+    for a in (127.0, 1.0, 2.5, 0.1171875, 3e-20, 254.0):
+        x = torch.zeros(16 * D)
+        halves = (torch.arange(127) + 0.5) * a / 127
+        x[:127], x[127:254] = halves, -halves
+        x[254:381] = torch.nextafter(halves.float(), torch.tensor(1e30))
+        x[381:508] = torch.nextafter(halves.float(), torch.tensor(0.0))
+        x = x.to(DT[dtype])
+        x[600] = a
+        x = x.clamp(-float(x[600]), float(x[600]))
+        c.k[0][0], c.v[0][0] = x.reshape(16, D), x.flip(0).reshape(16, D)
+        c.have = [0]
+        c.append([16])
+        c.check_cache()
+
+
+def test_rounding_to_e4m3():
+    """Every midpoint of two e4m3 values, its neighbours, subnormals and what rounds to zero, at several scales."""
+    val = R.e4m3_values()
+    mid = (val[1:] + val[:-1]) / 2
+    c = Case([16], 1, 1, 16, "e4m3", "f32", seed=7)
+    for scale in (1.0, 2.0 ** -20, 2.0 ** 30):
+        x = torch.zeros(16 * D, dtype=torch.float32)
+        m = (mid * scale).float()
+        parts = [m, -m, torch.nextafter(m, torch.tensor(1e38)), torch.nextafter(m, torch.tensor(0.0)), (val * scale).float(),
+                 torch.tensor([1e-30 * scale, 448.0 * scale])]
+        parts = torch.cat(parts)
+        x[: len(parts)] = parts
+        c.k[0][0], c.v[0][0] = x.reshape(16, D), -x.reshape(16, D)
+        c.have = [0]
+        c.append([16])
+        c.check_cache()
+    for a in (448.0, 449.0, 1.75, 1.7500001, 1.0, 0.9999999):   # the scale's own border
+        x = torch.randn(16 * D, generator=gen(8)).clamp(-a, a)
+        x[5] = a
+        c.k[0][0], c.v[0][0] = x.reshape(16, D), x.reshape(16, D)
+        c.have = [0]
+        c.append([16])
+        c.check_cache()
+
+
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+def test_blocks_of_zeros_tiny_and_not_finite(fmt):
+    c = Case([6 * 16], 1, 1, 16, fmt, "f32", seed=9)
+    k = c.k[0][0]
+    k[:16] = 0
+    k[16:32] *= 1e-32
+    k[32, 5] = math.inf
+    k[50, 7] = -math.inf
+    k[70, 9] = math.nan
+    k[80:96] *= 1e30
+    c.append([96])
+    torch.cuda.synchronize()
+    ks = c.cache.k_scale[0, 0].cpu()
+    codes = c.cache.k[0, 0].float().cpu().reshape(6, 16, D)
+    assert ks[0] == 0 and ks[1] == 0 and ks[2:5].isnan().all() and torch.isfinite(ks[5]) and ks[5] > 0
+    assert (codes[:5] == 0).all() and (codes[5] != 0).any()
+    bd = c.cache.bounds[0, 0].cpu()
+    assert bd[2, 1, 5] == math.inf and bd[3, 0, 7] == -math.inf and bd[4, :, 9].isnan().all()
+    assert torch.isfinite(bd[4, :, :9]).all()
+    assert torch.equal(bd[5, 1], k[80:96].amax(0))
+
+
+# ---------------------------------------------------------------------------------------------- block selection
+
+def run_select(c, shared, top, window, n_sink, tokens=False, lens=None, ws_fill=0xFF):
+    lens = c.have if lens is None else lens
+    H = c.kv_heads if shared else c.heads
+    cos_b, sin_b, _, _ = B.rope_tables(D, c.inv, 2048, 0, "cuda")
+    o = {"q_rot": torch.full((c.batch, c.heads, D), 9.0, device="cuda"),
+         "idx": torch.full((c.batch, H, top), -9, dtype=torch.int32, device="cuda"),
+         "count": torch.full((c.batch, H), -9, dtype=torch.int32, device="cuda"),
+         "score": torch.full((c.batch, H, top), 9.0, device="cuda")}
+    if tokens:
+        o["tokens"] = torch.full((c.batch, H, top * c.blk), -9, dtype=torch.int32, device="cuda")
+        o["n_tokens"] = torch.full((c.batch, H), -9, dtype=torch.int32, device="cuda")
+    ws = torch.full((max(16, B.workspace_bytes(c.dims, B.OP_BLOCK_TOPK)),), ws_fill, dtype=torch.uint8, device="cuda")
+    sl = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    B.block_topk(c.dims, c.cache, c.q.cuda(), cos_b, sin_b, o["q_rot"], shared, top, window, n_sink, sl, o["idx"], o["count"],
+                 o["score"], o.get("tokens"), o.get("n_tokens"), ws)
+    torch.cuda.synchronize()
+    o = {x: t.cpu() for x, t in o.items()}
+    q64 = R.rotate(c.q.double(), cos_b.cpu().double(), sin_b.cpu().double())
+    # float64 of either side may round to neighbours of each other: half a step, 2^-24, twice
+    assert (o["q_rot"].double() - q64).abs().max() <= 2.0 ** -23 * q64.abs().max()
+    return o
+
+
+def check_select(c, o, shared, top, window, n_sink, bounds=None):
+    for b in range(c.batch):
+        for kv in range(c.kv_heads):
+            n = c.have[b]
+            bd = c.seq(b, kv, n).bounds if bounds is None else bounds[b][kv]
+            q = o["q_rot"][b, kv * c.G:(kv + 1) * c.G].double()
+            for i, (blocks, score) in enumerate(R.select(q, bd, n, c.blk, window, n_sink, top, shared)):
+                h = kv if shared else kv * c.G + i
+                k = len(blocks)
+                assert int(o["count"][b, h]) == k, (b, h)
+                assert o["idx"][b, h].tolist() == blocks + [-1] * (top - k), (b, h)
+                assert torch.equal(o["score"][b, h, k:], torch.zeros(top - k))
+                # the same float64 sum in another order: at most a neighbouring float32
+                assert (o["score"][b, h, :k] - score).abs().max().item() <= 2.0 ** -23 * score.abs().max().item() if k else True
+                if "tokens" in o:
+                    t = R.tokens_of(blocks, n, c.blk, window, n_sink)
+                    assert int(o["n_tokens"][b, h]) == len(t)
+                    assert o["tokens"][b, h].tolist() == t + [-1] * (top * c.blk - len(t))
+
+
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("G", [1, 2, 3, 4, 5, 6, 7, 8])
+def test_select_every_group(G, shared):
+    c = Case([777, 50, 0], 2 * G, 2, 16, "i8", "bf16" if G % 2 else "f32", seed=20 + G)
+    c.append(c.lens)
+    o = run_select(c, shared, 9, 20, 3, tokens=True)
+    check_select(c, o, shared, 9, 20, 3)
+
+
+@pytest.mark.parametrize("blk, page, window, n_sink, top", [
+    (16, 0, 0, 0, 5), (32, 32, 1, 0, 200), (64, 128, 63, 70, 3), (128, 0, 130, 1, 2), (16, 64, 1000, 4, 4), (32, 0, 64, 4, 0),
+    (32, 0, 33, 31, 1), (16, 16, 17, 16, 30)])
+def test_select_edges(blk, page, window, n_sink, top):
+    """Windows and sinks that end inside a block, that leave no candidate, K above the candidates, K 0 and 1, pages,
+    sequences of no token, one, a block more or less one."""
+    c = Case([0, 1, blk - 1, blk, blk + 1, 700, 333], 4, 2, blk, "i8", "bf16", page, seed=blk + window)
+    c.append(c.lens)
+    for shared in (False, True):
+        o = run_select(c, shared, top, window, n_sink, tokens=top > 0)
+        check_select(c, o, shared, top, window, n_sink)
+
+
+def test_select_ties_go_to_the_lower_block():
+    """Blocks of only two kinds of keys: almost everything is tied."""
+    c = Case([40 * 16], 4, 2, 16, "i8", "f32", seed=31)
+    kinds = torch.randn(2, D, generator=gen(32))
+    pick = torch.randint(0, 2, (40,), generator=gen(33))
+    c.k[0][:] = kinds[pick].repeat_interleave(16, 0)
+    c.append([640])
+    for top in (1, 3, 17, 39, 40):
+        for shared in (False, True):
+            o = run_select(c, shared, top, 0, 0, tokens=True)
+            check_select(c, o, shared, top, 0, 0)
+
+
+@pytest.mark.parametrize("ctx, blk, top", [(1024 * 16, 16, 100), (1025 * 16, 16, 4096), (4096 * 16 + 5, 16, 129),
+                                           (16384 * 16 + 1, 16, 1000), (1 << 20, 16, 4096), (1 << 20, 128, 64)])
+def test_select_of_many_blocks(ctx, blk, top):
+    """Up to 65536 blocks of a head, on either side of what a thread keeps; bounds drawn directly."""
+    dims = dims_of(1, 2, 1, ctx, up(ctx, blk))
+    nb = -(-ctx // blk)
+    c = Case.__new__(Case)
+    c.batch, c.heads, c.kv_heads, c.G, c.blk, c.page, c.dims, c.have = 1, 2, 1, 2, blk, 0, dims, [ctx]
+    c.inv = synth.inv_freq(D, 500000.0)
+    g = gen(ctx % 1000 + blk)
+    c.q = torch.randn(1, 2, D, generator=g).bfloat16()
+    mid = torch.randn(nb, D, generator=g) * 0.5
+    bd = torch.stack([mid - 2, mid + 2], 1).bfloat16()
+    bd[100:120] = bd[100]                                  # some ties
+    full = torch.zeros(1, 1, up(ctx, blk) // blk, 2, D, dtype=torch.bfloat16)
+    full[0, 0, :nb] = bd
+    c.cache = B.KvBlocks(dims, blk, torch.bfloat16, bounds=full.cuda())
+    for shared in (False, True):
+        o = run_select(c, shared, top, 100, 3)
+        check_select(c, o, shared, top, 100, 3, bounds=[[bd.double()]])
+
+
+def test_select_survives_what_is_not_finite():
+    """K' blocks are selected whatever the scores are worth, and a score that is no number counts as infinite."""
+    c = Case([40 * 16], 2, 1, 16, "i8", "f32", seed=35)
+    c.k[0][0, 5 * 16 + 3, 7] = math.nan
+    c.k[0][0, 9 * 16 + 3, 7] = math.inf
+    c.append([640])
+    o = run_select(c, False, 4, 0, 0)
+    for h in range(2):
+        idx = o["idx"][0, h].tolist()
+        assert idx == sorted(idx) and len(set(idx)) == 4 and 5 in idx and int(o["count"][0, h]) == 4
+    c.q[:] = math.nan
+    sl = torch.tensor([640], dtype=torch.int32, device="cuda")
+    cos_b, sin_b, _, _ = B.rope_tables(D, c.inv, 2048, 0, "cuda")
+    idx = torch.full((1, 2, 4), -9, dtype=torch.int32, device="cuda")
+    cnt = torch.zeros(1, 2, dtype=torch.int32, device="cuda")
+    ws = torch.empty(B.workspace_bytes(c.dims, B.OP_BLOCK_TOPK), dtype=torch.uint8, device="cuda")
+    B.block_topk(c.dims, c.cache, c.q.cuda(), cos_b, sin_b, torch.empty(1, 2, D, device="cuda"), False, 4, 0, 0, sl, idx, cnt, ws=ws)
+    assert idx.cpu().tolist() == [[[0, 1, 2, 3]] * 2]
+
+
+# ---------------------------------------------------------------------------------------------- attention
+
+def run_attend(c, sel, size, shared, window, n_sink, ws_fill=0xFF, q_rot=None):
+    """sel [B, H] lists.  -> out (float64), q_rot."""
+    H = c.kv_heads if shared else c.heads
+    n_sel = max([len(x) for row in sel for x in row] + [1])
+    idx = torch.full((c.batch, H, n_sel), -1, dtype=torch.int32)
+    cnt = torch.zeros(c.batch, H, dtype=torch.int32)
+    for b in range(c.batch):
+        for h in range(H):
+            idx[b, h, : len(sel[b][h])] = torch.tensor(sel[b][h], dtype=torch.int32)
+            cnt[b, h] = len(sel[b][h])
+    cos_b, sin_b, cos_w, sin_w = B.rope_tables(D, c.inv, 2048, window, "cuda")
+    if q_rot is None:
+        q_rot = R.rotate(c.q.double(), cos_b.cpu().double(), sin_b.cpu().double()).float()
+    ws = torch.full((max(16, B.workspace_bytes(c.dims, B.OP_ATTN_KV8, n_sel * size, window)),), ws_fill, dtype=torch.uint8, device="cuda")
+    out = torch.full((c.batch, c.heads, D), 3.0, dtype=c.dtype, device="cuda")
+    sl = torch.tensor(c.have, dtype=torch.int32, device="cuda")
+    B.sparse_attn_kv8(c.dims, c.cache, c.q.cuda(), q_rot.cuda(), idx.cuda(), cnt.cuda(), n_sel, size, shared, window, n_sink,
+                      cos_w, sin_w, sl, out, ws)
+    torch.cuda.synchronize()
+    return out.cpu(), q_rot, cos_w.cpu().double(), sin_w.cpu().double()
+
+
+def check_attend(c, got, q_rot, cos_w, sin_w, sel, size, shared, window, n_sink):
+    half_step = 2.0 ** -8 if c.dtype == torch.bfloat16 else 2.0 ** -24
+    for b in range(c.batch):
+        n = c.have[b]
+        lo, hi = R.candidates(n, window, n_sink)
+        for h in range(c.heads):
+            kv = h // c.G
+            s = c.seq(b, kv, n)
+            picked = sel[b][kv if shared else h]
+            pos = [j for j in picked if lo <= j < hi] if size == 1 else R.tokens_of(picked, n, c.blk, window, n_sink)
+            want, off = R.attend(c.q[b, h].double(), q_rot[b, h].double(), s.rows["k"], s.rows["v"], n, pos, window, n_sink, cos_w, sin_w)
+            err = (got[b, h].double() - want).abs()
+            tol = off * (1 + half_step) + half_step * want.abs()
+            assert (err <= tol).all(), (b, h, float((err - tol).max()), float(err.max()))
+
+
+def draw_sel(c, size, shared, n_sel, window, n_sink, seed):
+    g = gen(seed)
+    H = c.kv_heads if shared else c.heads
+    sel = []
+    for b in range(c.batch):
+        lo, hi = R.candidates(c.have[b], window, n_sink)
+        units = list(range(lo // size, (hi - 1) // size + 1)) if hi > lo else []
+        row = []
+        for _ in range(H):
+            perm = torch.randperm(len(units), generator=g).tolist()[: n_sel]
+            row.append([units[i] for i in perm])          # (in any order)
+        sel.append(row)
+    return sel
+
+
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("blk, page, unit, window, n_sink, n_sel", [
+    (16, 0, 1, 64, 0, 100), (32, 64, 1, 5, 3, 40), (64, 0, 64, 0, 0, 3), (128, 128, 128, 20, 40, 2), (16, 32, 16, 300, 1, 7),
+    (32, 0, 1, 1, 700, 10)])
+@pytest.mark.parametrize("shared", [False, True])
+def test_attention(fmt, dtype, blk, page, unit, window, n_sink, n_sel, shared):
+    """Lengths around a block, short windows (so that selected rows lie in the incomplete block), sinks past the end."""
+    c = Case([0, 1, blk - 1, blk, blk + 1, 530], 6, 2, blk, fmt, dtype, page, seed=blk + n_sel, bounds=False)
+    c.append(c.lens)
+    sel = draw_sel(c, unit, shared, n_sel, window, n_sink, 40)
+    got = run_attend(c, sel, unit, shared, window, n_sink)
+    check_attend(c, *got, sel, unit, shared, window, n_sink)
+
+
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("G", [1, 2, 3, 4, 5, 7, 8])
+def test_attention_of_every_group(G, shared):
+    c = Case([901, 300], 2 * G, 2, 32, "i8" if G % 2 else "e4m3", "bf16" if G % 3 else "f32", seed=50 + G, bounds=False)
+    c.append(c.lens)
+    for unit, n_sel in ((1, 333), (32, 11)):
+        sel = draw_sel(c, unit, shared, n_sel, 48, 2, 51)
+        got = run_attend(c, sel, unit, shared, 48, 2)
+        check_attend(c, *got, sel, unit, shared, 48, 2)
+
+
+@pytest.mark.parametrize("batch, heads, kv_heads, n, n_sel, shared", [
+    (1, 4, 1, 5000, 4096, False), (1, 8, 1, 5000, 4096, True), (40, 8, 1, 700, 300, False), (70, 8, 8, 600, 256, True)])
+def test_attention_shared_out_or_not(batch, heads, kv_heads, n, n_sel, shared):
+    """Few heads of many rows (several workgroups a head, several tiles), and many heads of few."""
+    c = Case([n] * min(batch, 2) + [17] * (batch - min(batch, 2)), heads, kv_heads, 16, "i8", "f32", seed=60, bounds=False)
+    c.append(c.lens)
+    sel = draw_sel(c, 1, shared, n_sel, 100, 4, 61)
+    got = run_attend(c, sel, 1, shared, 100, 4)
+    check_attend(c, *got, sel, 1, shared, 100, 4)
+    again = run_attend(c, sel, 1, shared, 100, 4, ws_fill=0x00)
+    assert torch.equal(got[0], again[0])                    # the workspace's contents do not matter, nor the run
+
+
+@pytest.mark.parametrize("window", [0, 1, 700, 5000])
+def test_attention_of_the_window_alone(window):
+    c = Case([700, 3, 64, 0], 4, 4, 64, "e4m3", "bf16", seed=70, bounds=False)
+    c.append(c.lens)
+    sel = [[[] for _ in range(4)] for _ in range(4)]
+    got = run_attend(c, sel, 1, False, window, 0)
+    check_attend(c, *got, sel, 1, False, window, 0)
+    if window == 0:
+        assert (got[0] == 0).all()
+    assert (got[0][3] == 0).all()
+
+
+@pytest.mark.parametrize("unit", [1, 16])
+def test_indices_that_are_no_candidates_are_not_attended(unit):
+    c = Case([200, 90], 2, 1, 16, "i8", "f32", seed=71, bounds=False)
+    c.append(c.lens)
+    good = [7, 3] if unit == 16 else [100, 40, 33]
+    bad = [-1, -2147483648, 2147483647, 1 << 24, 200 // unit + 1, 199 // unit if unit == 1 else 13, 0 if unit == 1 else 12]
+    sel = [[good + bad] * 2, [[4] + bad] * 2]
+    keep = [[[j for j in s if R.tokens_of([j], n, unit, 20, 4)] if unit > 1 else s for s in row] for row, n in zip(sel, c.lens)]
+    keep = [[[j for j in s if 0 <= j <= (n - 1) // unit] for s in row] for row, n in zip(keep, c.lens)]
+    got = run_attend(c, sel, unit, False, 20, 4)
+    check_attend(c, *got, keep, unit, False, 20, 4)
+
+
+def test_what_is_not_finite_shows():
+    """A block with a value that is no number makes what attends it NaN, and nothing else."""
+    c = Case([96, 96], 2, 2, 16, "e4m3", "bf16", seed=72, bounds=False)
+    c.v[0][0, 20, 3] = math.nan
+    c.append(c.lens)
+    sel = [[[1], [1]], [[1], [1]]]
+    got = run_attend(c, sel, 16, False, 16, 0)[0]
+    assert got[0, 0].isnan().all() and torch.isfinite(got[0, 1]).all() and torch.isfinite(got[1]).all()
+    sel = [[[2], [1]], [[1], [1]]]
+    assert torch.isfinite(run_attend(c, sel, 16, False, 16, 0)[0]).all()
+
+
+def test_large_logits():
+    """Logits of some thousands: one row has all the weight."""
+    c = Case([400], 4, 1, 32, "i8", "f32", seed=73, bounds=False, spread=300.0)
+    c.append(c.lens)
+    sel = draw_sel(c, 1, False, 200, 40, 1, 74)
+    got = run_attend(c, sel, 1, False, 40, 1)
+    assert torch.isfinite(got[0]).all()
+    # with logits this far apart the bound of the other tests is larger than one: the winner's value row is what is left
+    for h in range(4):
+        s = c.seq(0, 0)
+        far = [0] + [j for j in sel[0][h] if 1 <= j < 360]
+        heads = got[1][0, h].double()
+        near = torch.arange(360, 400)
+        turned = R.rotate(c.q[0, h].double().expand(40, D), got[2][399 - near], got[3][399 - near])
+        logit = torch.cat([s.rows["k"][far] @ heads, (s.rows["k"][near] * turned).sum(-1)]) / math.sqrt(D)
+        top2 = logit.topk(2).values
+        if top2[0] - top2[1] > 30:
+            win = torch.cat([torch.tensor(far), near])[logit.argmax()]
+            assert (got[0][0, h].double() - s.rows["v"][win]).abs().max() <= 2.0 ** -20 * s.rows["v"][win].abs().max()
+
+
+# ---------------------------------------------------------------------------------------------- together
+
+@pytest.mark.parametrize("shared, page, dtype, fmt", [(False, 0, "bf16", "i8"), (True, 64, "f32", "e4m3")])
+def test_decode_steps(shared, page, dtype, fmt):
+    """Prefill, then tokens one by one over two block borders: append, select, attend, each against float64."""
+    lens = [230, 61]
+    c = Case(lens, 8, 2, 32, fmt, dtype, page, seed=80)
+    start = [160, 0]
+    c.append(start)
+    st = B.BlockDecodeState(c.dims, c.cache, 3, 20, 2, c.inv, 2048, shared)
+    steps = 70
+    lens_dev = torch.tensor(start, dtype=torch.int32, device="cuda")
+    for i in range(61):
+        lens_dev += 1
+        k = torch.stack([c.k[b][:, start[b] + i] for b in range(2)]).unsqueeze(2).contiguous().cuda()
+        v = torch.stack([c.v[b][:, start[b] + i] for b in range(2)]).unsqueeze(2).contiguous().cuda()
+        q = torch.randn(2, 8, D, generator=gen(1000 + i)).to(c.dtype)
+        out = st.step(q.cuda(), k, v, lens_dev)
+        c.have = [start[b] + i + 1 for b in range(2)]
+        if i in (0, 1, 2, 20, 29, 30, 31, 32, 33, 60):
+            c.q = q
+            torch.cuda.synchronize()
+            c.check_cache()
+            o = {"q_rot": st.q_rot.cpu(), "idx": st.block_idx.cpu(), "count": st.block_count.cpu(), "score": st.block_score.cpu()}
+            check_select(c, o, shared, 3, 20, 2)
+            H = 2 if shared else 8
+            sel = [[[j for j in o["idx"][b, h].tolist() if j >= 0] for h in range(H)] for b in range(2)]
+            check_attend(c, out.cpu(), o["q_rot"], st.cos_win.cpu().double(), st.sin_win.cpu().double(), sel, 32, shared, 20, 2)
+    assert steps > 61
+
+
+def test_captured_steps_replay():
+    """A step in a graph, replayed with other inputs and lengths, with eager work in between: every replay is the eager result."""
+    c = Case([300, 300], 8, 2, 16, "i8", "bf16", seed=81)
+    c.append([200, 130])
+    eager = Case([300, 300], 8, 2, 16, "i8", "bf16", seed=81)
+    eager.append([200, 130])
+    warm = Case([40, 40], 8, 2, 16, "i8", "bf16", seed=83)   # (the kernels are loaded before the capture)
+    sw = B.BlockDecodeState(warm.dims, warm.cache, 4, 24, 1, c.inv, 2048, False)
+    sw.step(warm.q.cuda(), *(torch.zeros(2, 2, 1, D, dtype=torch.bfloat16, device="cuda") for _ in range(2)),
+            torch.ones(2, dtype=torch.int32, device="cuda"))
+    st = B.BlockDecodeState(c.dims, c.cache, 4, 24, 1, c.inv, 2048, False)
+    se = B.BlockDecodeState(c.dims, eager.cache, 4, 24, 1, c.inv, 2048, False)
+    q = torch.zeros(2, 8, D, dtype=torch.bfloat16, device="cuda")
+    k, v = (torch.zeros(2, 2, 1, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    lens = torch.tensor([200, 130], dtype=torch.int32, device="cuda")
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        st.step(q, k, v, lens)
+    for i in range(20):
+        lens += 1
+        q.copy_(torch.randn(2, 8, D, generator=gen(i)).bfloat16())
+        k.copy_(torch.randn(2, 2, 1, D, generator=gen(100 + i)).bfloat16())
+        v.copy_(torch.randn(2, 2, 1, D, generator=gen(200 + i)).bfloat16())
+        graph.replay()
+        want = se.step(q, k, v, lens)
+        torch.cuda.synchronize()
+        assert torch.equal(st.out, want) and torch.equal(st.block_idx, se.block_idx)
+    for x in ("k_scale", "v_scale", "k_tail", "v_tail", "bounds"):
+        assert torch.equal(getattr(c.cache, x), getattr(eager.cache, x)), x
+    assert torch.equal(c.cache.k, eager.cache.k) and torch.equal(c.cache.v, eager.cache.v)
+
+
+def test_on_another_stream():
+    """Calls go to the current stream: work queued there before them is waited for, and two caches on two streams do not meet."""
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    cases = [Case([350, 77], 8, 2, 32, "i8", "bf16", seed=82 + i) for i in range(2)]
+    outs = []
+    for i, (c, s) in enumerate(zip(cases, streams)):
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            c.append(c.lens)
+            st = B.BlockDecodeState(c.dims, c.cache, 3, 10, 0, c.inv, 2048, True)
+            lens = torch.tensor(c.lens, dtype=torch.int32, device="cuda")
+            q = c.q.cuda()
+            B.block_topk(c.dims, c.cache, q, st.cos_b, st.sin_b, st.q_rot, True, 3, 10, 0, lens, st.block_idx, st.block_count,
+                         st.block_score, ws=st.ws)
+            B.sparse_attn_kv8(c.dims, c.cache, q, st.q_rot, st.block_idx, st.block_count, 3, 32, True, 10, 0, st.cos_win,
+                              st.sin_win, lens, st.out, st.ws)
+            outs.append((st, lens, q))
+    torch.cuda.synchronize()
+    for c, (st, _, _) in zip(cases, outs):
+        c.check_cache()
+        o = {"q_rot": st.q_rot.cpu(), "idx": st.block_idx.cpu(), "count": st.block_count.cpu(), "score": st.block_score.cpu()}
+        check_select(c, o, True, 3, 10, 0)
+        sel = [[[j for j in o["idx"][b, h].tolist() if j >= 0] for h in range(2)] for b in range(2)]
+        check_attend(c, st.out.cpu(), o["q_rot"], st.cos_win.cpu().double(), st.sin_win.cpu().double(), sel, 32, True, 10, 0)
+
+
+@pytest.mark.parametrize("shared", [False, True])
+def test_block_selection_for_a_cache_that_is_not_in_8_bits(shared):
+    """key_bounds + block_topk, whose token list is what a2ats_sparse_attn reads: the framework's own bfloat16 cache."""
+    blk, n, window, n_sink, top = 32, 500, 40, 3, 4
+    c = Case([n, n], 8, 2, blk, "i8", "bf16", seed=90)
+    cache = B.KvBlocks.empty(c.dims, blk, torch.bfloat16, codes=None)
+    cache.bounds.fill_(7.0)
+    done = 0
+    for m in (1, 30, 1, 1, 200, 267):                     # in pieces: 1, 31, 32, 33, 233, 500 tokens
+        sl = torch.full((2,), done + m, dtype=torch.int32, device="cuda")
+        B.key_bounds(c.dims, cache, torch.stack([k[:, done:done + m] for k in c.k]).contiguous().cuda(), m, sl)
+        done += m
+    torch.cuda.synchronize()
+    for b in range(2):
+        for kv in range(2):
+            assert torch.equal(cache.bounds[b, kv].cpu().double()[: -(-n // blk)], c.seq(b, kv).bounds)
+    c.cache, c.have = cache, [n, n]
+    o = run_select(c, shared, top, window, n_sink, tokens=True)
+    check_select(c, o, shared, top, window, n_sink)
+    kc, vc = (torch.zeros(2, 2, c.stride, D, dtype=torch.bfloat16) for _ in range(2))
+    for b in range(2):
+        kc[b, :, :n], vc[b, :, :n] = c.k[b], c.v[b]
+    _, _, cos_w, sin_w = B.rope_tables(D, c.inv, 2048, window, "cuda")
+    out = torch.empty(2, 8, D, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(B.workspace_bytes(c.dims, B.OP_ATTN, top * blk, window), dtype=torch.uint8, device="cuda")
+    call = B.sparse_attn_shared if shared else B.sparse_attn
+    call(c.dims, c.q.cuda(), o["q_rot"].cuda(), kc.cuda(), vc.cuda(), o["tokens"].cuda(), o["n_tokens"].cuda(), top * blk, window,
+         n_sink, cos_w, sin_w, None, out, ws)
+    torch.cuda.synchronize()
+    for b in range(2):
+        for h in range(8):
+            kv = h // 4
+            t = o["tokens"][b, kv if shared else h]
+            pos = t[t >= 0].tolist()
+            # (n == ctx_len: the call without lengths covers the rows before stride's padding)
+            want, off = R.attend(c.q[b, h].double(), o["q_rot"][b, h].double(), c.k[b][kv].double(), c.v[b][kv].double(), n, pos, window,
+                                 n_sink, cos_w.cpu().double(), sin_w.cpu().double())
+            err = (out[b, h].cpu().double() - want).abs()
+            # the shared form's queries are two bfloat16 terms: 2^-15 of a logit's terms as well, on a weight, twice, and
+            # sum p |v| is at most the largest |v|
+            terms = (o["q_rot"][b, h].double().abs() @ c.k[b][kv].double().abs().T).max() / math.sqrt(D)
+            more = 2 * 2.0 ** -15 * terms * c.v[b][kv].double().abs().max() if shared else 0.0
+            assert (err <= off + more + 2.0 ** -8 * (want.abs() + off)).all(), (b, h, float(err.max()))
+
+
+def test_a_pool_of_more_than_4_gib():
+    """Pages behind the first 2^32 bytes of a pool: append, select and attend there."""
+    page, blk, Hkv = 64, 32, 8
+    n_pages = (1 << 32) // (Hkv * page * D) + 300          # 5.2 GB in all of codes of keys, and as many of values
+    n = 300
+    slots = up(n, page) // page
+    dims = dims_of(1, 8, Hkv, n, up(n, page))
+    table = torch.arange(n_pages - 1, n_pages - 1 - 2 * slots, -2, dtype=torch.int32).reshape(1, slots).cuda()
+    cache = B.KvBlocks.empty(dims, blk, torch.bfloat16, torch.int8, True, table, page, n_pages)
+    c = Case([n], 8, Hkv, blk, "i8", "bf16", seed=95)
+    c.page, c.cache, c.dims = page, cache, dims
+    c.append([n], use_lens=False)
+    torch.cuda.synchronize()
+    for kv in (0, 7):
+        want = c.seq(0, kv)
+        rows = torch.cat([cache.k[p, kv] for p in table[0].tolist()]).cpu().double().reshape(-1, blk, D)
+        assert torch.equal(rows[: n // blk], want.codes["k"])
+    o = run_select(c, False, 3, 20, 2)
+    check_select(c, o, False, 3, 20, 2)
+    sel = [[o["idx"][0, h].tolist() for h in range(8)]]
+    got = run_attend(c, sel, blk, False, 20, 2, q_rot=o["q_rot"])
+    check_attend(c, *got, sel, blk, False, 20, 2)
