@@ -4,11 +4,21 @@
 // The scales are per row of a block, so they multiply the finished product and the weight, never the 128 elements.  Rows of
 // the sequence's incomplete block are in the tail, in the type of q.
 //
-// A row is 128 bytes of keys and as many of values, 2 flop per byte and head: a gather.  LPR lanes take a row, 128 / LPR
-// elements each; a wave works on 64 / LPR rows at once and has two sets of U of them, one requested while the other is used.
-// Each group of LPR lanes keeps its own running maximum, sum and accumulator, and one rescaling serves the U rows
-// of a set; the groups, then the waves, then (where a head's rows are shared out among workgroups) the workgroups are merged.
-// Logits are kept times log2 e, so that a weight is one exponential of a difference.
+// A row is 128 bytes of keys and as many of values, 2 flop per byte and head: a gather, whose instructions per row are what
+// has to stay below its bytes.  Both products are on the matrix cores, also for one head, with the 16 columns of a tile used for
+// the precision of the float32 operand:
+//   - keys (A, 16 rows x 128) times queries (B).  A column is (head, term): int8 keys go into v_mfma_i32_16x16x64_i8 as they
+//     come from memory, the query as three signed digits to the base 256 of q * 2^(22 - e), |q| < 2^e, so that a logit is an
+//     exact integer sum; e4m3 keys become float16 (exact) and the query two float16 terms.  The terms of a head are added
+//     across the columns of a lane row.
+//   - values (A, 16 dimensions x 32 rows) times weights (B).  Logits leave the first product with a head in each column and
+//     four rows of each of two tiles in each lane, which is the B operand of the second as it stands: no exchange between lanes.
+//     Weights are split into bfloat16 terms by truncation, again a column each: the range of float32 stays (v_scale is in the
+//     weight), and 16 bits (8 heads, bfloat16 output) to 24 bits (else) of precision.  A lane loads 8 bytes of each of its
+//     8 rows; the dimensions of tile t are 8 n + t, so that the transposition is a choice of bytes within a lane.
+// Window rows are turned back by their distance, (q R_delta) . k = q . (k R_-delta), and go in as two float16 terms.  What is
+// left in the tail, at most a block, is done on the vector ALU.
+// The statistics, all sums and the output are float32.  Logits are kept times log2 e, so that a weight is one exponential.
 #include <algorithm>
 #include <cfloat>
 
@@ -19,52 +29,61 @@ namespace a2ats {
 namespace {
 
 constexpr int kD = kRowBytes;
-constexpr int kThreads = 512, kWaves = kThreads / 64;
-constexpr int kTile = 2048;            // far rows staged in LDS at a time
-constexpr float kNone = -FLT_MAX;      // the maximum of no rows
-constexpr float kLogit = 0.12751743f;  // log2(e) / sqrt(128)
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kPair = 32;               // rows that a wave takes at a time: two tiles of 16
+constexpr float kNone = -FLT_MAX;       // the maximum of no rows
+constexpr float kLogit = 0.12751743f;   // log2(e) / sqrt(128)
+
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 
 __device__ __forceinline__ float power(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Sum over aligned groups of 8 or 16 lanes, in every lane.
-template <int LPR>
-__device__ __forceinline__ float group_sum(float v) {
-  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xf, 0xf, false));    // quad_perm [1,0,3,2]
-  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xf, 0xf, false));    // quad_perm [2,3,0,1]
-  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xf, 0xf, false));   // row_half_mirror
-  if (LPR == 16) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xf, 0xf, false));   // row_mirror
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+// Sum over the columns of a head, c, c + GP, .. of 16, in every lane.
+template <int GP>
+__device__ __forceinline__ float head_sum(float v) {
+  if (GP == 4) v += dpp<0x124>(v);   // row_ror:4
+  v += dpp<0x128>(v);                // row_ror:8
+  return v;
+}
+// Over the four lane rows, in every lane.
+template <typename F>
+__device__ __forceinline__ float over_rows(float v, F f) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float rows_max(float v) {
+  return over_rows(v, [](float x, float y) { return fmaxf(x, y); });
+}
+__device__ __forceinline__ float rows_sum(float v) {
+  return over_rows(v, [](float x, float y) { return x + y; });
+}
+// Sum over aligned groups of 8 lanes, in every lane.
+__device__ __forceinline__ float group8_fsum(float v) {
+  v += dpp<0xB1>(v);    // quad_perm [1,0,3,2]
+  v += dpp<0x4E>(v);    // quad_perm [2,3,0,1]
+  v += dpp<0x141>(v);   // row_half_mirror
   return v;
 }
 
-// The four codes of a word as floats.
-template <bool E4M3>
-__device__ __forceinline__ void widen4(uint32_t w, float* x) {
-  if (E4M3) {
-    const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-    x[0] = a[0]; x[1] = a[1]; x[2] = b[0]; x[3] = b[1];
-  } else {
-    x[0] = (float)(int8_t)(w & 255u);
-    x[1] = (float)(int8_t)((w >> 8) & 255u);
-    x[2] = (float)(int8_t)((w >> 16) & 255u);
-    x[3] = (float)(int8_t)(w >> 24);
-  }
+__device__ __forceinline__ float code_float(uint32_t w, int byte) {   // of int8
+  return (float)(int8_t)((w >> (8 * byte)) & 255u);
 }
-template <bool E4M3, int W>
-__device__ __forceinline__ void widen_words(const uint32_t (&w)[W], float (&x)[4 * W]) {
-#pragma unroll
-  for (int i = 0; i < W; ++i) widen4<E4M3>(w[i], x + 4 * i);
+// The upper halves of two floats, the first one below: bfloat16 by truncation.
+__device__ __forceinline__ uint32_t upper_halves(float a, float b) {
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
 }
-template <int W>
-__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[W]) {
-  if constexpr (W == 4) {
-    const uint4 v = *(const uint4*)p;
-    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-  } else {
-    const uint2 v = *(const uint2*)p;
-    w[0] = v.x; w[1] = v.y;
-  }
-}
-// Half of DPL consecutive elements of a row in the type of q.
+__device__ __forceinline__ uint32_t f16_bits(f16x2 v) { return __builtin_bit_cast(uint32_t, v); }
+
 template <int N>
 __device__ __forceinline__ void load_elems(const float* p, float* x) {
 #pragma unroll
@@ -76,44 +95,44 @@ __device__ __forceinline__ void load_elems(const float* p, float* x) {
 template <int N>
 __device__ __forceinline__ void load_elems(const uint16_t* p, float* x) {
 #pragma unroll
-  for (int i = 0; i < N; i += 4) {
-    const uint2 v = *(const uint2*)(p + i);
-    x[i] = __uint_as_float(v.x << 16); x[i + 1] = __uint_as_float(v.x & 0xffff0000u);
-    x[i + 2] = __uint_as_float(v.y << 16); x[i + 3] = __uint_as_float(v.y & 0xffff0000u);
+  for (int i = 0; i < N; i += 8) {
+    float y[8];
+    load8(p + i, y);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[i + e] = y[e];
   }
 }
 __device__ __forceinline__ void store_elem(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_elem(uint16_t* p, float v) { *p = f32_to_bf16(v); }
 
-// Running softmax of GH heads over the rows of a group of lanes; DPL output elements a lane.
-template <int GH, int DPL>
-struct State {
-  float m[GH], l[GH], o[GH][DPL];
-  __device__ __forceinline__ void clear() {
+// The least e >= -100 with |x| < 2^e for all x of a head's row (32 elements in this lane, the others in the lane rows);
+// ok: all are finite.
+__device__ __forceinline__ int row_exponent(const float (&x)[32], bool& ok) {
+  uint32_t big = 0;
 #pragma unroll
-    for (int g = 0; g < GH; ++g) {
-      m[g] = kNone;
-      l[g] = 0.f;
-#pragma unroll
-      for (int e = 0; e < DPL; ++e) o[g][e] = 0.f;
-    }
-  }
-};
+  for (int i = 0; i < 32; ++i) big = max(big, __float_as_uint(x[i]) & 0x7fffffffu);
+  const auto a = __builtin_amdgcn_permlane32_swap(big, big, false, false);
+  big = max(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane16_swap(big, big, false, false);
+  big = max(b[0], b[1]);
+  ok = big < 0x7f800000u;
+  return max((int)(big >> 23) - 126, -100);
+}
 
-// One row more for every head: `x` its values, `logit` (times log2 e) for each head.
-template <int GH, int DPL>
-__device__ __forceinline__ void absorb(State<GH, DPL>& st, const float (&logit)[GH], bool in, float scale, const float (&x)[DPL]) {
+// A query as float16 terms, for the columns of the first two: x = 2^e (hi + lo), to 2^-22 of 2^e.  Returns 2^e.
+__device__ __forceinline__ float query_terms(const float (&x)[32], int term, bool active, f16x8 (&q)[4]) {
+  bool ok;
+  const int e = row_exponent(x, ok);
+  const float down = ldexpf(active && term < 2 ? 1.f : 0.f, -e);   // (2^-128 is a subnormal number, and exact)
+  const float less = term == 1 ? 1.f : 0.f;
 #pragma unroll
-  for (int g = 0; g < GH; ++g) {
-    const float lg = in ? logit[g] : kNone;
-    const float mn = fmaxf(st.m[g], lg);
-    const float alpha = power(st.m[g] - mn), p = in ? power(lg - mn) : 0.f;
-    st.l[g] = st.l[g] * alpha + p;
-    const float pv = p * scale;
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int e = 0; e < DPL; ++e) st.o[g][e] = st.o[g][e] * alpha + pv * x[e];
-    st.m[g] = mn;
-  }
+    for (int j = 0; j < 8; ++j) {
+      const float y = x[8 * i + j] * down;
+      q[i][j] = (_Float16)(y - less * (float)(_Float16)y);
+    }
+  return ok ? ldexpf(1.f, e) : __uint_as_float(0x7fc00000u);
 }
 
 struct AttnArgs {
@@ -127,318 +146,635 @@ struct AttnArgs {
   const int32_t* seq_lens;
   float* partial;
   void* out;
-  int32_t ctx_len, n_sel, sel_shift, window, n_sink, group, parts, win_waves, problems;
+  int32_t ctx_len, n_sel, sel_shift, window, n_sink, group, shared, problems;
+  int32_t parts, far_share, win_share;   // workgroups of a head's (KV head's) rows, and how many of them each takes
 };
 
-// E4M3: format of the codes.  GH: heads that attend the same rows, G of a KV head padded to 1, 2, 4 or 8 (shared selection),
-// or 1.  LPR: lanes of a row.
-template <typename T, bool E4M3, int GH, bool SHARED>
-__global__ __launch_bounds__(kThreads) void attn_kv8_kernel(AttnArgs a) {
-  constexpr int LPR = GH > 4 ? 16 : 8, DPL = kD / LPR, W = DPL / 4, SLOTS = 64 / LPR;
-  constexpr int U = GH == 1 ? 4 : 2;
-  __shared__ uint32_t s_row[kTile];   // row of the cache, from the first one of the base block up (or kNoRow)
-  __shared__ float s_ks[kTile], s_vs[kTile];
-  __shared__ uint32_t s_late[4];      // selected rows of the incomplete block
-  __shared__ float s_m[kWaves][GH], s_l[kWaves][GH], s_o[kWaves][GH][kD];
-  constexpr uint32_t kNoRow = 0xffffffffu;
+// The rows of a pair of tiles as they come from memory: keys of row `column` of either tile, 32 elements; values of the rows
+// 4 * lane row + 0 .. 3 of either, 8 elements.
+struct PairRows {
+  uint4 k[2][2];
+  uint2 v[8];
+};
+// Where the rows of two pairs are in the cache, their scales, and 0 or, for a place without a row, -inf: of a wave, in LDS.
+struct PairPlaces {
+  uint32_t row[2 * kPair];
+  float ks[2 * kPair], vs[2 * kPair], none[2 * kPair];
+};
 
-  // All workgroups of a KV head run on one XCD, whose L2 then serves the rows that its heads have in common.
-  const int G = a.group, per = SHARED ? a.parts : a.parts * G;
-  int prob, pg;
-  xcd_map(blockIdx.x, per, a.problems, prob, pg);
-  const int Hkv = a.cache.n_kv_heads, b = prob / Hkv, kv = prob % Hkv;
-  const int part = SHARED ? pg : pg / G, h0 = SHARED ? 0 : pg % G;
-  const int head = prob * G + h0;                 // the first of the workgroup's heads
-  const int sel = SHARED ? prob : head;           // whose selection it reads
-  const int tid = threadIdx.x, lane = tid & 63, slot = lane / LPR, sub = lane % LPR;
-  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const SeqRange sr = seq_range(a.ctx_len, a.seq_lens, b, a.window, a.n_sink, 0);
-  const int shift = a.cache.shift, blk = 1 << shift, tail0 = sr.n >> shift << shift;
-  const int cnt = min(max(a.sel_count[sel], 0), a.n_sel);
-  const int32_t* idx = a.sel_idx + (size_t)sel * a.n_sel;
-  const T* kt = (const T*)a.cache.k_tail + ((size_t)prob << shift) * kD;
-  const T* vt = (const T*)a.cache.v_tail + ((size_t)prob << shift) * kD;
+// A wave's running softmax: a head in each column (the same m in all lane rows, l of the lane's own rows), and its output,
+// o[t][i] being dimension 8 * (4 * lane row + i) + t.
+struct WaveState {
+  float m, l;
+  f32x4 o[8];
+};
 
-  // This part's share of the far rows (sinks, then the selected ones) and of the window.
-  const int far_all = sr.sink_end + (cnt << a.sel_shift), win_all = sr.n - sr.win_start;
-  const int f0 = (int)((long)far_all * part / a.parts), f1 = (int)((long)far_all * (part + 1) / a.parts);
-  const int w0 = sr.win_start + (int)((long)win_all * part / a.parts);
-  const int w1 = sr.win_start + (int)((long)win_all * (part + 1) / a.parts);
-
-  State<GH, DPL> st;
-  st.clear();
-  const int far_waves = kWaves - a.win_waves;
-  const bool far_role = wv < far_waves;
-  // Elements of this lane: far rows DPL consecutive ones; window rows DPL / 2 of each half, which are turned together.
-  constexpr int HD = DPL / 2;
-  const int d_far = sub * DPL, d_win = sub * HD;
-  float qv[GH][DPL];
+__device__ __forceinline__ void load_keys(const uint8_t* k, const uint32_t* rows, int col, int at, int step, PairRows& p) {
 #pragma unroll
-  for (int g = 0; g < GH; ++g) {
-    const int hg = head + (GH > 1 ? min(g, G - 1) : 0);
-    if (far_role) {
-      load_elems<DPL>(a.q_rot + (size_t)hg * kD + d_far, qv[g]);
-    } else {
-      load_elems<HD>((const T*)a.q + (size_t)hg * kD + d_win, qv[g]);
-      load_elems<HD>((const T*)a.q + (size_t)hg * kD + kD / 2 + d_win, qv[g] + HD);
+  for (int t = 0; t < 2; ++t) {
+    const uint32_t r = rows[t * 16 + col];
+    const uint8_t* from = k + (size_t)r * kRowBytes + at;
+    p.k[t][0] = *(const uint4*)from;
+    p.k[t][1] = *(const uint4*)(from + step);
+  }
+}
+__device__ __forceinline__ void load_values(const uint8_t* v, const uint32_t* rows, int col, int lrow, PairRows& p) {
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const uint4 r4 = *(const uint4*)(rows + t * 16 + lrow * 4);
+    const uint32_t r[4] = {r4.x, r4.y, r4.z, r4.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p.v[4 * t + i] = *(const uint2*)(v + (size_t)r[i] * kRowBytes + col * 8);
+  }
+}
+
+// The weights of the two tiles' rows of a lane, from their products with the queries (times log2 e / sqrt(128), without the keys'
+// scales), times v_scale; the state's maximum and sum.
+__device__ __forceinline__ void pair_weights(const f32x4 (&dot)[2], const PairPlaces& pl, int first, int lrow, WaveState& st,
+                                             float (&w)[8]) {
+  float lg[8], vsc[8];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int at = first + t * 16 + lrow * 4;
+    const float4 k4 = *(const float4*)(pl.ks + at), v4 = *(const float4*)(pl.vs + at), n4 = *(const float4*)(pl.none + at);
+    const float kk[4] = {k4.x, k4.y, k4.z, k4.w}, vv[4] = {v4.x, v4.y, v4.z, v4.w}, nn[4] = {n4.x, n4.y, n4.z, n4.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      lg[4 * t + i] = __builtin_fmaf(dot[t][i], kk[i], nn[i]);
+      vsc[4 * t + i] = vv[i];
     }
   }
-  if (tid < 4) s_late[tid] = 0u;
+  float mx = lg[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) mx = fmaxf(mx, lg[i]);
+  const float mn = fmaxf(st.m, rows_max(mx));
+  if (__builtin_amdgcn_ballot_w64(mn > st.m)) {
+    const float alpha = power(st.m - mn);
+    st.l *= alpha;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) st.o[t] *= alpha;
+    st.m = mn;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float p = power(lg[i] - mn);
+    st.l += p;
+    w[i] = p * vsc[i];
+  }
+}
 
-  const int tiles = max(1, (f1 - f0 + kTile - 1) / kTile);
-  for (int tile = 0; tile < tiles; ++tile) {
-    const int t0 = f0 + tile * kTile, tn = min(kTile, f1 - t0);
-    __syncthreads();
-    for (int i = tid; i < tn; i += kThreads) {
-      const int t = t0 + i;
-      int j = t;
-      bool in = true;
-      if (t >= sr.sink_end) {
-        const int s = t - sr.sink_end;
-        const int unit = idx[s >> a.sel_shift];
-        in = unit >= 0 && unit <= (sr.n - 1) >> a.sel_shift;   // (an index from elsewhere must not leave the cache)
-        j = in ? (unit << a.sel_shift) + (s & ((1 << a.sel_shift) - 1)) : 0;
-        in = in && j >= sr.sink_end && j < sr.win_start;
-      }
-      if (in && j >= tail0) {
-        atomicOr(&s_late[(j - tail0) >> 5], 1u << ((j - tail0) & 31));
-        in = false;
-      }
-      uint32_t row = kNoRow;
-      float ks = 0.f, vs = 0.f;
-      if (in) {
-        const size_t at = block_at(a.cache, b, kv, j >> shift);
-        row = (uint32_t)((at << shift) + (size_t)(j & (blk - 1)));
-        ks = a.cache.k_scale[at] * kLogit;
-        vs = a.cache.v_scale[at];
-      }
-      s_row[i] = row;
-      s_ks[i] = ks;
-      s_vs[i] = vs;
+// The pair's values times its weights.
+template <bool E4M3, int GP, bool EXACT>
+__device__ __forceinline__ void absorb_values(const float (&weight)[8], int term, const PairRows& p, WaveState& st) {
+  // The weights' terms: a column takes its own.
+  const uint32_t cut1 = term >= 1 ? 0xffff0000u : 0u, cut2 = term >= 2 ? 0xffff0000u : 0u;
+  float x[8], rest[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float y = weight[i];
+    if (GP == 8 && EXACT) {
+      const float y1 = y - __uint_as_float(__float_as_uint(y) & 0xffff0000u);
+      rest[i] = y1 - __uint_as_float(__float_as_uint(y1) & 0xffff0000u);
     }
-    __syncthreads();
-    if (far_role && tn > 0) {
-      const int rb = far_waves * SLOTS, step = rb * U, first = wv * SLOTS + slot;
-      uint32_t ka[U][W], va[U][W], kc[U][W], vc[U][W];
-      auto load_set = [&](int i0, uint32_t (&kr)[U][W], uint32_t (&vr)[U][W]) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const uint32_t row = s_row[min(i0 + u * rb, tn - 1)];
-          const size_t off = (size_t)(row == kNoRow ? 0u : row) * kRowBytes + d_far;
-          load_words<W>(a.cache.k + off, kr[u]);
-          load_words<W>(a.cache.v + off, vr[u]);
-        }
-      };
-      auto use_set = [&](int i0, const uint32_t (&kr)[U][W], uint32_t (&vr)[U][W]) {
-        float lg[U][GH], vs[U];
-        bool in[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int i = min(i0 + u * rb, tn - 1);
-          in[u] = i0 + u * rb < tn && s_row[i] != kNoRow;
-          vs[u] = s_vs[i];
-          const float ks = s_ks[i];
-          float kf[DPL];
-          widen_words<E4M3, W>(kr[u], kf);
-#pragma unroll
-          for (int g = 0; g < GH; ++g) {
-            float dot = 0.f;
-#pragma unroll
-            for (int e = 0; e < DPL; ++e) dot += qv[g][e] * kf[e];
-            dot = group_sum<LPR>(dot) * ks;
-            lg[u][g] = in[u] ? dot : kNone;
-          }
-        }
-        float pv[U][GH];
-#pragma unroll
-        for (int g = 0; g < GH; ++g) {
-          float mn = st.m[g];
-#pragma unroll
-          for (int u = 0; u < U; ++u) mn = fmaxf(mn, lg[u][g]);
-          const float alpha = power(st.m[g] - mn);
-          st.m[g] = mn;
-          float l = st.l[g] * alpha;
-#pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const float p = in[u] ? power(lg[u][g] - mn) : 0.f;
-            l += p;
-            pv[u][g] = in[u] ? p * vs[u] : 0.f;
-          }
-          st.l[g] = l;
-#pragma unroll
-          for (int e = 0; e < DPL; ++e) st.o[g][e] *= alpha;
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          float vf[DPL];
-          if (E4M3) {   // (what is read for no row may be a NaN)
-#pragma unroll
-            for (int i = 0; i < W; ++i) vr[u][i] = in[u] ? vr[u][i] : 0u;
-          }
-          widen_words<E4M3, W>(vr[u], vf);
-#pragma unroll
-          for (int g = 0; g < GH; ++g)
-#pragma unroll
-            for (int e = 0; e < DPL; ++e) st.o[g][e] += pv[u][g] * vf[e];
-        }
-      };
-      load_set(first, ka, va);
-#pragma unroll 1
-      for (int base = 0; base < tn; base += 2 * step) {
-        load_set(base + step + first, kc, vc);
-        use_set(base + first, ka, va);
-        load_set(base + 2 * step + first, ka, va);
-        use_set(base + step + first, kc, vc);
-      }
-    }
-    if (!far_role && tile == 0) {
-      // Window rows: the key is turned back by the row's distance, once for all heads:  (q R_delta) . k = q . (k R_-delta).
-      const int rb = a.win_waves * SLOTS;
-      auto turned = [&](int j, const float (&kf)[DPL], float (&lg)[GH], float ks) {
-        const int delta = min(max(sr.n - 1 - j, 0), a.window - 1);
-        const float* cp = a.cos_win + (size_t)delta * (kD / 2) + d_win;
-        const float* sp = a.sin_win + (size_t)delta * (kD / 2) + d_win;
-        float cs[HD], sn[HD], kr[DPL];
-        load_elems<HD>(cp, cs);
-        load_elems<HD>(sp, sn);
-#pragma unroll
-        for (int e = 0; e < HD; ++e) {
-          kr[e] = kf[e] * cs[e] + kf[HD + e] * sn[e];
-          kr[HD + e] = kf[HD + e] * cs[e] - kf[e] * sn[e];
-        }
-#pragma unroll
-        for (int g = 0; g < GH; ++g) {
-          float dot = 0.f;
-#pragma unroll
-          for (int e = 0; e < DPL; ++e) dot += qv[g][e] * kr[e];
-          lg[g] = group_sum<LPR>(dot) * ks;
-        }
-      };
-      const int w8 = min(w1, max(w0, tail0));   // [w0, w8) in 8 bits, [w8, w1) in the tail
-      for (int j0 = w0 + (wv - far_waves) * SLOTS; j0 < w8; j0 += rb) {
-        const int j = j0 + slot, jc = min(j, w8 - 1);
-        const size_t at = block_at(a.cache, b, kv, jc >> shift);
-        const size_t off = ((at << shift) + (size_t)(jc & (blk - 1))) * kRowBytes + d_win;
-        uint32_t kw[2][W / 2], vw[2][W / 2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if constexpr (W == 4) {
-            load_words<2>(a.cache.k + off + h * (kD / 2), kw[h]);
-            load_words<2>(a.cache.v + off + h * (kD / 2), vw[h]);
-          } else {
-            kw[h][0] = *(const uint32_t*)(a.cache.k + off + h * (kD / 2));
-            vw[h][0] = *(const uint32_t*)(a.cache.v + off + h * (kD / 2));
-          }
-        }
-        float kf[DPL], vf[DPL], lg[GH];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int i = 0; i < W / 2; ++i) {
-            widen4<E4M3>(kw[h][i], kf + h * HD + 4 * i);
-            widen4<E4M3>(vw[h][i], vf + h * HD + 4 * i);
-          }
-        turned(jc, kf, lg, a.cache.k_scale[at] * kLogit);
-        absorb<GH, DPL>(st, lg, j < w8, a.cache.v_scale[at], vf);
-      }
-      for (int j0 = w8 + (wv - far_waves) * SLOTS; j0 < w1; j0 += rb) {
-        const int j = j0 + slot, jc = min(j, w1 - 1);
-        const size_t off = (size_t)(jc & (blk - 1)) * kD + d_win;
-        float kf[DPL], vf[DPL], lg[GH];
-        load_elems<HD>(kt + off, kf);
-        load_elems<HD>(kt + off + kD / 2, kf + HD);
-        load_elems<HD>(vt + off, vf);
-        load_elems<HD>(vt + off + kD / 2, vf + HD);
-        turned(jc, kf, lg, kLogit);
-        absorb<GH, DPL>(st, lg, j < w1, 1.f, vf);
-      }
-    }
+    y -= __uint_as_float(__float_as_uint(y) & cut1);
+    if (GP == 4) y -= __uint_as_float(__float_as_uint(y) & cut2);
+    x[i] = y;
   }
-  // Far rows of the incomplete block (only where the window is shorter than that block).
-  __syncthreads();
-  if (wv == 0 && (s_late[0] | s_late[1] | s_late[2] | s_late[3]) != 0u) {
-    for (int r0 = 0; r0 < sr.n - tail0; r0 += SLOTS) {
-      const int r = min(r0 + slot, sr.n - 1 - tail0);
-      const bool in = r0 + slot < sr.n - tail0 && (s_late[r >> 5] >> (r & 31) & 1u);
-      float kf[DPL], vf[DPL], lg[GH];
-      load_elems<DPL>(kt + (size_t)r * kD + d_far, kf);
-      load_elems<DPL>(vt + (size_t)r * kD + d_far, vf);
+  uint32_t pw[4], rw[4];
 #pragma unroll
-      for (int g = 0; g < GH; ++g) {
-        float dot = 0.f;
+  for (int i = 0; i < 4; ++i) {
+    pw[i] = upper_halves(x[2 * i], x[2 * i + 1]);
+    if (GP == 4) pw[i] = term == 3 ? 0u : pw[i];
+    if (GP == 8 && EXACT) rw[i] = term == 0 ? upper_halves(rest[2 * i], rest[2 * i + 1]) : 0u;
+  }
+  const bf16x8 pb = __builtin_bit_cast(bf16x8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
 #pragma unroll
-        for (int e = 0; e < DPL; ++e) dot += qv[g][e] * kf[e];
-        lg[g] = group_sum<LPR>(dot) * kLogit;
+  for (int h = 0; h < 2; ++h) {
+    // tiles 4 h + t: byte t of word h of the eight rows
+    uint32_t r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = h ? p.v[i].y : p.v[i].x;
+    uint32_t quad[2][4];   // e4m3: byte t of four rows
+    if (E4M3) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t u0 = __builtin_amdgcn_perm(r[4 * i + 1], r[4 * i], 0x05010400u);
+        const uint32_t u1 = __builtin_amdgcn_perm(r[4 * i + 1], r[4 * i], 0x07030602u);
+        const uint32_t u2 = __builtin_amdgcn_perm(r[4 * i + 3], r[4 * i + 2], 0x05010400u);
+        const uint32_t u3 = __builtin_amdgcn_perm(r[4 * i + 3], r[4 * i + 2], 0x07030602u);
+        quad[i][0] = __builtin_amdgcn_perm(u2, u0, 0x05040100u);
+        quad[i][1] = __builtin_amdgcn_perm(u2, u0, 0x07060302u);
+        quad[i][2] = __builtin_amdgcn_perm(u3, u1, 0x05040100u);
+        quad[i][3] = __builtin_amdgcn_perm(u3, u1, 0x07060302u);
       }
-      absorb<GH, DPL>(st, lg, in, 1.f, vf);
     }
-  }
-
-  // The groups of a wave take the wave's maximum and are added up.
 #pragma unroll
-  for (int g = 0; g < GH; ++g) {
-    float m = st.m[g];
+    for (int t = 0; t < 4; ++t) {
+      uint32_t w[4];
 #pragma unroll
-    for (int off = LPR; off < 64; off <<= 1) m = fmaxf(m, __shfl_xor(m, off));
-    const float f = power(st.m[g] - m);
-    float l = st.l[g] * f;
-#pragma unroll
-    for (int off = LPR; off < 64; off <<= 1) l += __shfl_xor(l, off);
-#pragma unroll
-    for (int e = 0; e < DPL; ++e) {
-      float o = st.o[g][e] * f;
-#pragma unroll
-      for (int off = LPR; off < 64; off <<= 1) o += __shfl_xor(o, off);
-      const int d = far_role ? d_far + e : (e < HD ? d_win + e : kD / 2 + d_win + e - HD);
-      if (slot == 0) s_o[wv][g][d] = o;
-    }
-    if (lane == 0) {
-      s_m[wv][g] = m;
-      s_l[wv][g] = l;
-    }
-  }
-  __syncthreads();
-  for (int i = tid; i < GH * kD; i += kThreads) {
-    const int g = i / kD, d = i % kD;
-    if (GH > 1 && g >= G) break;
-    float m = s_m[0][g];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) m = fmaxf(m, s_m[w][g]);
-    float l = 0.f, o = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float f = power(s_m[w][g] - m);
-      l += s_l[w][g] * f;
-      o += s_o[w][g][d] * f;
-    }
-    if (a.parts == 1) {
-      store_elem((T*)a.out + (size_t)(head + g) * kD + d, l == 0.f ? 0.f : o / l);
-    } else {
-      float* p = a.partial + ((size_t)(head + g) * a.parts + part) * (kD + 2);
-      p[d] = o;
-      if (d == 0) {
-        p[kD] = m;
-        p[kD + 1] = l;
+      for (int i = 0; i < 4; ++i) {
+        if (E4M3) {
+          w[i] = __builtin_bit_cast(uint32_t, (i & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(quad[i >> 1][t], 1.f, true)
+                                                      : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(quad[i >> 1][t], 1.f, false));
+        } else {
+          w[i] = upper_halves(code_float(r[2 * i], t), code_float(r[2 * i + 1], t));   // (exact)
+        }
+      }
+      const bf16x8 vt = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+      st.o[4 * h + t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pb, st.o[4 * h + t], 0, 0, 0);
+      if (GP == 8 && EXACT) {
+        const bf16x8 rb = __builtin_bit_cast(bf16x8, make_uint4(rw[0], rw[1], rw[2], rw[3]));
+        st.o[4 * h + t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, rb, st.o[4 * h + t], 0, 0, 0);
       }
     }
   }
 }
 
-// Merges the parts of a head, a thread per output element.
+// The queries of far rows as the second operand: int8 caches, three digits of eight bits; e4m3, two float16 terms.
+template <bool E4M3, int GP>
+struct FarQuery {
+  i32x4 d[E4M3 ? 1 : 2], d2[GP == 8 && !E4M3 ? 2 : 1];   // (eight heads: the third digit by itself)
+  f16x8 f[E4M3 ? 4 : 1];
+  float cw, cw2;   // what a column's product is worth
+  // Elements 32 * lane row + 0 .. 31 of the column's head.
+  __device__ __forceinline__ void set(const float (&x)[32], int term, bool active) {
+    cw2 = 0.f;
+    if constexpr (E4M3) {
+      cw = query_terms(x, term, active, f) * kLogit;
+    } else {
+      bool ok;
+      const int e = row_exponent(x, ok);
+      // v = rint(x 2^(22 - e)) is the low bits of x 2^(22 - e) + 3 * 2^22; v = (d0 256 + d1) 256 + d2 with signed digits:
+      // d2 = v, d1 = (v + 0x80) >> 8, d0 = (v + 0x8080) >> 16, the low 8 bits of each.
+      const float up = ldexpf(active ? 1.f : 0.f, 22 - e);
+      const uint32_t magic = 0x4b400000u, shift = term == 0 ? 16u : (term == 1 ? 8u : 0u);
+      const uint32_t bias = (term == 0 ? 0x8080u : (term == 1 ? 0x80u : 0u)) - magic;
+      const uint32_t mask = term == 3 ? 0u : 0xffu, mask2 = term == 0 ? 0xffu : 0u;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        uint32_t w = 0u, w2 = 0u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t v = __float_as_uint(__builtin_fmaf(x[4 * i + j], up, 12582912.f));
+          w |= (((v + bias) >> shift) & mask) << (8 * j);
+          if (GP == 8) w2 |= (v & mask2) << (8 * j);
+        }
+        d[i / 4][i % 4] = (int)w;
+        if constexpr (GP == 8) d2[i / 4][i % 4] = (int)w2;
+      }
+      cw = ok ? ldexpf(kLogit, e - 22 + (int)shift) : __uint_as_float(0x7fc00000u);
+      if (GP == 8) cw2 = ldexpf(kLogit, e - 22);
+    }
+  }
+  // Products of a tile's keys (32 elements of row `column`) with the queries: rows 4 * lane row + i.
+  __device__ __forceinline__ f32x4 dot(const uint4 (&k)[2]) const {
+    f32x4 r;
+    if constexpr (E4M3) {
+      const uint32_t w[8] = {k[0].x, k[0].y, k[0].z, k[0].w, k[1].x, k[1].y, k[1].z, k[1].w};
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint4 k4 = make_uint4(f16_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[2 * i], 1.f, false)),
+                                    f16_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[2 * i], 1.f, true)),
+                                    f16_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[2 * i + 1], 1.f, false)),
+                                    f16_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[2 * i + 1], 1.f, true)));
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, k4), f[i], acc, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[i] = head_sum<GP>(acc[i]) * cw;
+    } else {
+      i32x4 acc = {0, 0, 0, 0};
+      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, k[0]), d[0], acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, k[1]), d[1], acc, 0, 0, 0);
+      if constexpr (GP == 8) {
+        i32x4 acc2 = {0, 0, 0, 0};
+        acc2 = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, k[0]), d2[0], acc2, 0, 0, 0);
+        acc2 = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, k[1]), d2[1], acc2, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = head_sum<GP>((float)acc[i] * cw + (float)acc2[i] * cw2);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = head_sum<GP>((float)acc[i] * cw);
+      }
+    }
+    return r;
+  }
+};
+
+// Products of a tile's window keys (elements 16 * lane row + 0 .. 15 of either half of row `column`), turned back by the row's
+// angles, with the queries' float16 terms.
+template <bool E4M3>
+__device__ __forceinline__ f32x4 turned_dot(const uint4 (&k)[2], const float (&cs)[16], const float (&sn)[16], const f16x8 (&q)[4]) {
+  const uint32_t lw[4] = {k[0].x, k[0].y, k[0].z, k[0].w}, uw[4] = {k[1].x, k[1].y, k[1].z, k[1].w};
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {   // eight pairs of elements
+    float lower[8], upper[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t wl = lw[2 * i + (j >> 2)], wu = uw[2 * i + (j >> 2)];
+      float kl, ku;
+      if (E4M3) {
+        const auto dl = (j & 2) ? __builtin_amdgcn_cvt_pk_f32_fp8((int)wl, true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)wl, false);
+        const auto du = (j & 2) ? __builtin_amdgcn_cvt_pk_f32_fp8((int)wu, true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)wu, false);
+        kl = dl[j & 1];
+        ku = du[j & 1];
+      } else {
+        kl = code_float(wl, j & 3);
+        ku = code_float(wu, j & 3);
+      }
+      lower[j] = kl * cs[8 * i + j] + ku * sn[8 * i + j];
+      upper[j] = ku * cs[8 * i + j] - kl * sn[8 * i + j];
+    }
+    auto terms = [&](const float (&x)[8], const f16x8& qt) {
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const auto h = __builtin_amdgcn_cvt_pkrtz(x[2 * j], x[2 * j + 1]);
+        const auto r = __builtin_amdgcn_cvt_pkrtz(x[2 * j] - (float)h[0], x[2 * j + 1] - (float)h[1]);
+        hi[j] = __builtin_bit_cast(uint32_t, h);
+        lo[j] = __builtin_bit_cast(uint32_t, r);
+      }
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, make_uint4(hi[0], hi[1], hi[2], hi[3])), qt, acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, make_uint4(lo[0], lo[1], lo[2], lo[3])), qt, acc, 0, 0, 0);
+    };
+    terms(lower, q[i]);
+    terms(upper, q[2 + i]);
+  }
+  return acc;
+}
+
+// E4M3: format of the codes.  GP: heads that attend the same rows (one, or the G of a KV head if the selection is shared), padded to
+// 4 or 8: 16 / GP columns a head.
+template <typename T, bool E4M3, int GP>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3, 3))) void attn_kv8_kernel(AttnArgs a) {
+  constexpr bool EXACT = sizeof(T) == 4;
+  __shared__ union {
+    struct {
+      PairPlaces far[kWaves], win[kWaves];
+    } places;
+    float o[kWaves][GP][kD];
+  } s;
+  __shared__ float s_m[kWaves][GP], s_l[kWaves][GP], s_tm[8], s_tl[8], s_to[8][kD];
+  __shared__ uint32_t s_late[4];                   // selected rows of the incomplete block
+
+  // All workgroups of a KV head run on one XCD, whose L2 then serves the rows that its heads have in common.
+  const int G = a.group, nh = a.shared ? G : 1, per = a.shared ? a.parts : a.parts * G;
+  int prob, pg;
+  xcd_map(blockIdx.x, per, a.problems, prob, pg);
+  const int Hkv = a.cache.n_kv_heads, b = prob / Hkv, kv = prob % Hkv;
+  const int part = a.shared ? pg : pg / G;
+  const int head = prob * G + (a.shared ? 0 : pg % G);   // the first of the workgroup's heads
+  const int sel = a.shared ? prob : head;                // whose selection it reads
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, lrow = lane >> 4;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int32_t* idx = a.sel_idx + (size_t)sel * a.n_sel;
+
+  // This part's share of the far rows: row t is sink t, then row t - n_sink of the selection.  Places without a row are left
+  // out: what a part has to fetch first does not depend on the sequence's length.
+  const int n_sink = min(a.n_sink, a.ctx_len);
+  const int f0 = part * a.far_share;
+  auto unit_of = [&](int t) {   // (clamped: requested before it is known to count)
+    return a.n_sel > 0 ? idx[min(max(t - n_sink, 0) >> a.sel_shift, a.n_sel - 1)] : 0;
+  };
+
+  const SeqRange sr = seq_range(a.ctx_len, a.seq_lens, b, a.window, a.n_sink, 0);
+  const int shift = a.cache.shift, blk = 1 << shift, tail0 = sr.n >> shift << shift;
+  const int cnt = min(max(a.sel_count[sel], 0), a.n_sel);
+  const int f1 = min(f0 + a.far_share, n_sink + (cnt << a.sel_shift));
+  // ... and of the window: [w0, w8) in 8 bits, [w8, w1) in the tail.
+  const int w0 = min(sr.win_start + part * a.win_share, sr.n), w1 = min(w0 + a.win_share, sr.n);
+  const int w8 = min(w1, max(w0, tail0));
+  const int n_far = f1 > f0 ? (f1 - f0 + kPair - 1) / kPair : 0, n_win = (w8 - w0 + kPair - 1) / kPair;
+  // Wave by wave, the pairs win_first, win_first + kWaves, .. of the window, and of the far rows a stretch, so that all waves have
+  // about as much to do: a pair of the window is as much as two others.  Which wave of the SIMDs is the first goes by the
+  // workgroup (the waves with the window would else be on one SIMD in all workgroups of a CU).
+  const int win_first = (wv + (int)(blockIdx.x >> 3) + (int)(blockIdx.x >> 8)) & (kWaves - 1);
+  const int quota = (2 * n_win + n_far + kWaves - 1) / kWaves;
+  int far_first = 0, far_end = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const int take = max(quota - 2 * ((n_win - w + kWaves - 1) / kWaves), 0);   // (n_win + kWaves > w)
+    far_first += w < win_first ? take : 0;
+    far_end += w <= win_first ? take : 0;
+  }
+  far_first = min(far_first, n_far);
+  far_end = min(far_end, n_far);
+  // Lane l places row l % 32 of a pair (l < 32) or of the next one.
+  auto far_row = [&](int pair) { return f0 + pair * kPair + lane; };
+  int unit = unit_of(far_row(far_first));
+
+  // This lane's column: a head, and which term of its query and weights.
+  const int hd = col % GP, term = col / GP;
+  const bool active = hd < nh;
+  const size_t q_at = (size_t)(head + min(hd, nh - 1)) * kD;
+
+  if (tid < 4) s_late[tid] = 0u;
+  __syncthreads();
+  if (tail0 == 0) {   // no row is in 8 bits yet
+    for (int t = f0 + tid; t < f1; t += kThreads) {
+      int j = t;
+      if (t >= n_sink) {
+        const int u = idx[(t - n_sink) >> a.sel_shift];
+        j = u >= 0 && u <= (sr.n - 1) >> a.sel_shift ? (u << a.sel_shift) + ((t - n_sink) & ((1 << a.sel_shift) - 1)) : -1;
+        if (j < sr.sink_end || j >= sr.win_start) continue;
+      }
+      if (j < sr.win_start) atomicOr(&s_late[j >> 5], 1u << (j & 31));
+    }
+  }
+
+  // Where this lane's row is, and its scales, which are requested here and put beside it by put_scales.
+  struct Place {
+    size_t at;
+    float ks, vs;
+    bool in;
+  };
+  auto place = [&](PairPlaces& to, int j, bool in) {   // row j of the sequence
+    Place pc;
+    pc.in = in;
+    j = in ? j : 0;   // (a place without a row: the sequence's first one, which has been written and counts for nothing)
+    pc.at = block_at(a.cache, b, kv, j >> shift);
+    to.row[lane] = (uint32_t)((pc.at << shift) + (size_t)(j & (blk - 1)));
+    return pc;
+  };
+  auto get_scales = [&](Place& pc) {
+    pc.ks = a.cache.k_scale[pc.at];
+    pc.vs = a.cache.v_scale[pc.at];
+  };
+  auto put_scales = [&](PairPlaces& to, const Place& pc) {
+    to.ks[lane] = pc.in ? pc.ks : 0.f;
+    to.vs[lane] = pc.in ? pc.vs : 0.f;
+    to.none[lane] = pc.in ? 0.f : -INFINITY;
+  };
+  PairPlaces &pl = s.places.far[wv], &wp = s.places.win[wv];
+  auto place_far = [&](int pair) {   // this pair and the next one
+    const int t = far_row(pair);
+    bool in = t < f1;
+    int j = t;
+    if (t >= n_sink) {
+      in = in && unit >= 0 && unit <= (sr.n - 1) >> a.sel_shift;   // (an index from elsewhere must not leave the cache)
+      j = in ? (unit << a.sel_shift) + ((t - n_sink) & ((1 << a.sel_shift) - 1)) : 0;
+      in = in && j >= sr.sink_end && j < sr.win_start;
+    } else {
+      in = in && t < sr.sink_end;
+    }
+    if (in && j >= tail0) {
+      atomicOr(&s_late[(j - tail0) >> 5], 1u << ((j - tail0) & 31));
+      in = false;
+    }
+    return place(pl, j, in);
+  };
+  auto place_win = [&](int pair) {
+    const int j = w0 + pair * kPair + lane;
+    return place(wp, j, lane < kPair && j < w8);
+  };
+
+  // A wave takes its pairs of the window, then those of the far rows.  All that does not depend on other loads is requested
+  // first; then the next pair's keys are requested when the last one's have been multiplied, its values when those have been.
+  const bool has_far = far_first < far_end && tail0 > 0;
+  WaveState st;
+  PairRows p;
+  Place far_place;
+  st.m = kNone;
+  st.l = 0.f;
+#pragma unroll
+  for (int t = 0; t < 8; ++t) st.o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (win_first < n_win) {
+    float x[32];
+    load_elems<16>((const T*)a.q + q_at + lrow * 16, x);
+    load_elems<16>((const T*)a.q + q_at + kD / 2 + lrow * 16, x + 16);
+    Place win_place = place_win(win_first);
+    if (has_far) far_place = place_far(far_first);
+    get_scales(win_place);
+    if (has_far) get_scales(far_place);
+    load_keys(a.cache.k, wp.row, col, lrow * 16, kD / 2, p);
+    load_values(a.cache.v, wp.row, col, lrow, p);
+    f16x8 qw[4];
+    const float ww = query_terms(x, term, active, qw) * kLogit;
+    if (has_far) put_scales(pl, far_place);
+#pragma unroll 1
+    for (int pair = win_first; pair < n_win; pair += kWaves) {
+      f32x4 dot[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int delta = min(max(sr.n - 1 - (w0 + pair * kPair + t * 16 + col), 0), a.window - 1);
+        float cs[16], sn[16];
+        load_elems<16>(a.cos_win + (size_t)delta * (kD / 2) + lrow * 16, cs);
+        load_elems<16>(a.sin_win + (size_t)delta * (kD / 2) + lrow * 16, sn);
+        const f32x4 acc = turned_dot<E4M3>(p.k[t], cs, sn, qw);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dot[t][i] = head_sum<GP>(acc[i]) * ww;
+      }
+      put_scales(wp, win_place);
+      float w[8];
+      pair_weights(dot, wp, 0, lrow, st, w);
+      const bool more = pair + kWaves < n_win;
+      if (more) {
+        win_place = place_win(pair + kWaves);
+        get_scales(win_place);
+        load_keys(a.cache.k, wp.row, col, lrow * 16, kD / 2, p);
+      } else if (has_far) {
+        load_keys(a.cache.k, pl.row, col, lrow * 32, 16, p);
+      }
+      absorb_values<E4M3, GP, EXACT>(w, term, p, st);
+      if (more || has_far) load_values(a.cache.v, more ? wp.row : pl.row, col, lrow, p);
+    }
+  }
+  if (has_far) {
+    FarQuery<E4M3, GP> fq;
+    float x[32];
+    load_elems<32>(a.q_rot + q_at + lrow * 32, x);
+    if (win_first >= n_win) {
+      far_place = place_far(far_first);
+      get_scales(far_place);
+      load_keys(a.cache.k, pl.row, col, lrow * 32, 16, p);
+      load_values(a.cache.v, pl.row, col, lrow, p);
+      put_scales(pl, far_place);
+    }
+    unit = unit_of(far_row(far_first + 2));
+    fq.set(x, term, active);
+    int half = 0;
+#pragma unroll 1
+    for (int pair = far_first; pair < far_end; ++pair) {
+      f32x4 dot[2];
+      dot[0] = fq.dot(p.k[0]);
+      dot[1] = fq.dot(p.k[1]);
+      float w[8];
+      pair_weights(dot, pl, half * kPair, lrow, st, w);
+      const bool more = pair + 1 < far_end, again = half == 1 && more;
+      if (again) {
+        far_place = place_far(pair + 1);
+        get_scales(far_place);
+      }
+      const uint32_t* next = pl.row + (half ^ 1) * kPair;
+      if (more) load_keys(a.cache.k, next, col, lrow * 32, 16, p);
+      absorb_values<E4M3, GP, EXACT>(w, term, p, st);
+      if (more) load_values(a.cache.v, next, col, lrow, p);
+      if (again) {
+        put_scales(pl, far_place);
+        unit = unit_of(far_row(pair + 3));
+      }
+      half ^= 1;
+    }
+  }
+  __syncthreads();   // (the places are written again, with the outputs)
+
+  // The incomplete block: window rows of this part, and selected rows where the window is shorter than that block.  Up to
+  // four heads share out the waves, eight heads go to the four in turn.
+  const int wph = nh > 2 ? 1 : kWaves / nh;
+  const bool late = (s_late[0] | s_late[1] | s_late[2] | s_late[3]) != 0u, has_tail = late || w8 < w1;
+  if (has_tail) {
+#pragma unroll 1
+    for (int g = wv / wph; g < (GP == 8 ? 8 : kWaves / wph); g += kWaves) {
+      const int at_slot = GP == 8 ? g : wv;
+      float m = kNone, l = 0.f, o[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[e] = 0.f;
+      const int slot = lane >> 3, sub = lane & 7;
+      if (g < nh) {
+        const T* kt = (const T*)a.cache.k_tail + ((size_t)prob << shift) * kD;
+        const T* vt = (const T*)a.cache.v_tail + ((size_t)prob << shift) * kD;
+        float qr[16], qv[16];   // elements 8 * sub + 0 .. 7 of either half
+        const size_t at = (size_t)(head + g) * kD;
+        load_elems<8>((const T*)a.q + at + sub * 8, qv);
+        load_elems<8>((const T*)a.q + at + kD / 2 + sub * 8, qv + 8);
+        load_elems<8>(a.q_rot + at + sub * 8, qr);
+        load_elems<8>(a.q_rot + at + kD / 2 + sub * 8, qr + 8);
+        const int r_first = late ? 0 : w8 - tail0, r_end = late ? sr.n - tail0 : w1 - tail0;
+#pragma unroll 1
+        for (int r0 = r_first + (wv % wph) * 8; r0 < r_end; r0 += wph * 8) {
+          const int r = min(r0 + slot, r_end - 1), j = tail0 + r;
+          const bool win = j >= w8 && j < w1;
+          const bool in = r0 + slot < r_end && (win || (j < sr.win_start && (s_late[r >> 5] >> (r & 31) & 1u)));
+          float k[16], v[16], cs[8], sn[8];
+          load_elems<8>(kt + (size_t)r * kD + sub * 8, k);
+          load_elems<8>(kt + (size_t)r * kD + kD / 2 + sub * 8, k + 8);
+          load_elems<16>(vt + (size_t)r * kD + sub * 16, v);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) { cs[e] = 1.f; sn[e] = 0.f; }
+          if (win) {
+            const int delta = min(sr.n - 1 - j, a.window - 1);
+            load8(a.cos_win + (size_t)delta * (kD / 2) + sub * 8, cs);
+            load8(a.sin_win + (size_t)delta * (kD / 2) + sub * 8, sn);
+          }
+          float dot = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float q0 = win ? qv[e] : qr[e], q1 = win ? qv[8 + e] : qr[8 + e];
+            dot += q0 * (k[e] * cs[e] + k[8 + e] * sn[e]);
+            dot += q1 * (k[8 + e] * cs[e] - k[e] * sn[e]);
+          }
+          dot = group8_fsum(dot);
+          const float lg = in ? dot * kLogit : -INFINITY;
+          const float mn = fmaxf(m, lg), alpha = power(m - mn), pr = power(lg - mn);
+          l = l * alpha + pr;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[e] = o[e] * alpha + (in ? pr * v[e] : 0.f);
+          m = mn;
+        }
+        float mw = m;
+#pragma unroll
+        for (int off = 8; off < 64; off <<= 1) mw = fmaxf(mw, __shfl_xor(mw, off));
+        const float f = power(m - mw);
+        l *= f;
+#pragma unroll
+        for (int off = 8; off < 64; off <<= 1) l += __shfl_xor(l, off);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          o[e] *= f;
+#pragma unroll
+          for (int off = 8; off < 64; off <<= 1) o[e] += __shfl_xor(o[e], off);
+        }
+        m = mw;
+      }
+      if (slot == 0) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s_to[at_slot][sub * 16 + e] = o[e];
+      }
+      if (lane == 0) {
+        s_tm[at_slot] = m;
+        s_tl[at_slot] = l;
+      }
+    }
+  }
+
+  // The terms of a head are added up, and the waves merged.
+  const float l_all = rows_sum(st.l);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float o[8];
+#pragma unroll
+    for (int t = 0; t < 8; ++t) o[t] = head_sum<GP>(st.o[t][i]);
+    if (term == 0) {
+      float* to = &s.o[wv][hd][8 * (4 * lrow + i)];
+      *(float4*)to = make_float4(o[0], o[1], o[2], o[3]);
+      *(float4*)(to + 4) = make_float4(o[4], o[5], o[6], o[7]);
+    }
+  }
+  if (lane < GP) {
+    s_m[wv][lane] = st.m;
+    s_l[wv][lane] = l_all;
+  }
+  __syncthreads();
+  for (int i = tid; i < nh * kD; i += kThreads) {
+    const int g = i / kD, d = i % kD;
+    float m = kNone, l = 0.f, o = 0.f;
+    if (has_tail) {
+      const int t0 = GP == 8 ? g : g * wph, tn = GP == 8 ? 1 : wph;
+      for (int w = t0; w < t0 + tn; ++w) m = fmaxf(m, s_tm[w]);
+      for (int w = t0; w < t0 + tn; ++w) {
+        const float f = power(s_tm[w] - m);
+        l += s_tl[w] * f;
+        o += s_to[w][d] * f;
+      }
+    }
+    float mn = m;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) mn = fmaxf(mn, s_m[w][g]);
+    const float f = power(m - mn);
+    l *= f;
+    o *= f;
+    m = mn;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = power(s_m[w][g] - m);
+      l += s_l[w][g] * f;
+      o += s.o[w][g][d] * f;
+    }
+    if (a.parts == 1) {
+      store_elem((T*)a.out + (size_t)(head + g) * kD + d, l == 0.f ? 0.f : o / l);
+    } else {
+      float* to = a.partial + ((size_t)(head + g) * a.parts + part) * (kD + 2);
+      to[d] = o;
+      if (d == 0) {
+        to[kD] = m;
+        to[kD + 1] = l;
+      }
+    }
+  }
+}
+
+// Merges the parts of a head, at most 32, a thread per output element.
 template <typename T>
 __global__ __launch_bounds__(kD) void attn_kv8_merge_kernel(const float* __restrict__ partial, T* __restrict__ out, int parts) {
   const float* p = partial + (size_t)blockIdx.x * parts * (kD + 2);
-  const int d = threadIdx.x;
-  float m = kNone;
-  for (int i = 0; i < parts; ++i) m = fmaxf(m, p[(size_t)i * (kD + 2) + kD]);
-  float l = 0.f, o = 0.f;
-#pragma unroll 8
-  for (int i = 0; i < parts; ++i) {
-    const float* s = p + (size_t)i * (kD + 2);
-    const float f = power(s[kD] - m);
-    l += s[kD + 1] * f;
-    o += s[d] * f;
-  }
+  const int d = threadIdx.x, lane = d & 63;
+  const float* mine = p + (size_t)min(lane, parts - 1) * (kD + 2) + kD;
+  const float mp = mine[0], lp = mine[1];
+  float o8[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) o8[i] = p[(size_t)min(i, parts - 1) * (kD + 2) + d];
+  float m = mp;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) m = fmaxf(m, __shfl_xor(m, off));
+  const float f = lane < parts ? power(mp - m) : 0.f;
+  float l = f * (lane < parts ? lp : 0.f), o = 0.f;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) l += __shfl_xor(l, off);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) o += i < parts ? __shfl(f, i) * o8[i] : 0.f;
+  for (int i = 8; i < parts; ++i) o += __shfl(f, i) * p[(size_t)i * (kD + 2) + d];
+  l = __shfl(l, 0);
   store_elem(out + (size_t)blockIdx.x * kD + d, l == 0.f ? 0.f : o / l);
 }
 
@@ -448,22 +784,19 @@ Kv8Plan make_kv8_plan(const a2ats_dims& d, long sel_rows, int window, bool share
   Kv8Plan p;
   const long problems = (long)d.batch * (shared ? d.n_kv_heads : d.n_q_heads);
   const long rows = std::min<long>(sel_rows, d.ctx_len) + std::min(window, d.ctx_len);
-  // Two workgroups a CU, each with 128 rows at least (16 a wave).
+  // Two workgroups a CU, each with a pair of tiles at least for every wave.
   long parts = problems > 0 ? (512 + problems - 1) / problems : 1;
-  parts = std::max(1l, std::min(std::min(parts, rows / 128), 32l));
+  parts = std::max(1l, std::min(std::min(parts, rows / (kWaves * kPair)), 32l));
   p.parts = (int)parts;
   p.bytes = parts > 1 ? (size_t)d.batch * d.n_q_heads * parts * (kD + 2) * sizeof(float) : 0;
   return p;
 }
 
 template <typename T, bool E4M3>
-static void launch_heads(const AttnArgs& a, bool shared, long workgroups, hipStream_t stream) {
+static void launch_heads(const AttnArgs& a, long workgroups, hipStream_t stream) {
   const dim3 grid((unsigned)workgroups), block(kThreads);
-  if (!shared) hipLaunchKernelGGL((attn_kv8_kernel<T, E4M3, 1, false>), grid, block, 0, stream, a);
-  else if (a.group == 1) hipLaunchKernelGGL((attn_kv8_kernel<T, E4M3, 1, true>), grid, block, 0, stream, a);
-  else if (a.group == 2) hipLaunchKernelGGL((attn_kv8_kernel<T, E4M3, 2, true>), grid, block, 0, stream, a);
-  else if (a.group <= 4) hipLaunchKernelGGL((attn_kv8_kernel<T, E4M3, 4, true>), grid, block, 0, stream, a);
-  else hipLaunchKernelGGL((attn_kv8_kernel<T, E4M3, 8, true>), grid, block, 0, stream, a);
+  if (a.shared && a.group > 4) hipLaunchKernelGGL((attn_kv8_kernel<T, E4M3, 8>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((attn_kv8_kernel<T, E4M3, 4>), grid, block, 0, stream, a);
 }
 
 hipError_t launch_sparse_attn_kv8(const a2ats_dims& d, const BlockCache& m, int kv_dtype, int format, const void* q,
@@ -489,20 +822,20 @@ hipError_t launch_sparse_attn_kv8(const a2ats_dims& d, const BlockCache& m, int 
   a.window = window;
   a.n_sink = n_sink;
   a.group = d.n_q_heads / d.n_kv_heads;
+  a.shared = shared;
   a.parts = p.parts;
+  const long far = ((long)n_sel << sel_shift) + std::min(n_sink, d.ctx_len), win = std::min(window, d.ctx_len);
+  a.far_share = (int)((far + p.parts - 1) / p.parts);
+  a.win_share = (int)((win + p.parts - 1) / p.parts);
   a.problems = d.batch * d.n_kv_heads;
-  // Waves for the window in proportion to its rows, which cost about half as much again as others.
-  const long far = std::min<long>(((long)n_sel << sel_shift) + n_sink, d.ctx_len), win = 3l * std::min(window, d.ctx_len);
-  const long all = std::max(1l, 2 * far + win);
-  a.win_waves = window == 0 ? 0 : std::min(kWaves - 1, std::max(1, (int)((kWaves * win + all / 2) / all)));
   const long workgroups = (long)a.problems * p.parts * (shared ? 1 : a.group);
   const bool e4m3 = format == A2ATS_E4M3;
   if (kv_dtype == A2ATS_BF16) {
-    if (e4m3) launch_heads<uint16_t, true>(a, shared, workgroups, stream);
-    else launch_heads<uint16_t, false>(a, shared, workgroups, stream);
+    if (e4m3) launch_heads<uint16_t, true>(a, workgroups, stream);
+    else launch_heads<uint16_t, false>(a, workgroups, stream);
   } else {
-    if (e4m3) launch_heads<float, true>(a, shared, workgroups, stream);
-    else launch_heads<float, false>(a, shared, workgroups, stream);
+    if (e4m3) launch_heads<float, true>(a, workgroups, stream);
+    else launch_heads<float, false>(a, workgroups, stream);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.parts == 1) return e;
