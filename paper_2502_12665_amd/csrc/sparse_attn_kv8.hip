@@ -162,6 +162,15 @@ struct PairPlaces {
   float ks[2 * kPair], vs[2 * kPair], none[2 * kPair];
 };
 
+// Eight rows of the incomplete block, one for each group of 8 lanes, and a head's query for them: elements 8 * (lane of the group)
+// + 0 .. 7 of either half of keys and query, 16 * (lane of the group) + 0 .. 15 of the values.
+struct TailRows {
+  float q[16], k[16], v[16], cs[8], sn[8];
+};
+struct TailState {
+  float m, l, o[16];
+};
+
 // A wave's running softmax: a head in each column (the same m in all lane rows, l of the lane's own rows), and its output,
 // o[t][i] being dimension 8 * (4 * lane row + i) + t.
 struct WaveState {
@@ -407,11 +416,11 @@ __device__ __forceinline__ f32x4 turned_dot(const uint4 (&k)[2], const float (&c
 // E4M3: format of the codes.  GP: heads that attend the same rows (one, or the G of a KV head if the selection is shared), padded to
 // 4 or 8: 16 / GP columns a head.
 template <typename T, bool E4M3, int GP>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3, 3))) void attn_kv8_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_kv8_kernel(AttnArgs a) {
   constexpr bool EXACT = sizeof(T) == 4;
   __shared__ union {
     struct {
-      PairPlaces far[kWaves], win[kWaves];
+      PairPlaces far[kWaves][2], win[kWaves];
     } places;
     float o[kWaves][GP][kD];
   } s;
@@ -442,9 +451,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3, 3))
   const int shift = a.cache.shift, blk = 1 << shift, tail0 = sr.n >> shift << shift;
   const int cnt = min(max(a.sel_count[sel], 0), a.n_sel);
   const int f1 = min(f0 + a.far_share, n_sink + (cnt << a.sel_shift));
-  // ... and of the window: [w0, w8) in 8 bits, [w8, w1) in the tail.
-  const int w0 = min(sr.win_start + part * a.win_share, sr.n), w1 = min(w0 + a.win_share, sr.n);
-  const int w8 = min(w1, max(w0, tail0));
+  // ... and of the window's rows in 8 bits, [w0, w8).
+  const int w0 = sr.win_start + part * a.win_share, w8 = max(w0, min(w0 + a.win_share, tail0));
   const int n_far = f1 > f0 ? (f1 - f0 + kPair - 1) / kPair : 0, n_win = (w8 - w0 + kPair - 1) / kPair;
   // Wave by wave, the pairs win_first, win_first + kWaves, .. of the window, and of the far rows a stretch, so that all waves have
   // about as much to do: a pair of the window is as much as two others.  Which wave of the SIMDs is the first goes by the
@@ -506,8 +514,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3, 3))
     to.vs[lane] = pc.in ? pc.vs : 0.f;
     to.none[lane] = pc.in ? 0.f : -INFINITY;
   };
-  PairPlaces &pl = s.places.far[wv], &wp = s.places.win[wv];
-  auto place_far = [&](int pair) {   // this pair and the next one
+  PairPlaces &wp = s.places.win[wv], *fp = s.places.far[wv];
+  auto place_far = [&](PairPlaces& to, int pair) {   // this pair and the next one
     const int t = far_row(pair);
     bool in = t < f1;
     int j = t;
@@ -522,36 +530,111 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3, 3))
       atomicOr(&s_late[(j - tail0) >> 5], 1u << ((j - tail0) & 31));
       in = false;
     }
-    return place(pl, j, in);
+    return place(to, j, in);
   };
   auto place_win = [&](int pair) {
     const int j = w0 + pair * kPair + lane;
     return place(wp, j, lane < kPair && j < w8);
   };
 
-  // A wave takes its pairs of the window, then those of the far rows.  All that does not depend on other loads is requested
-  // first; then the next pair's keys are requested when the last one's have been multiplied, its values when those have been.
-  const bool has_far = far_first < far_end && tail0 > 0;
+  // The rows of the incomplete block are done on the vector ALU, eight at a time.  Up to four heads share out the waves, eight
+  // heads go to the four in turn; the window's rows are dealt out to the parts.
+  const int wph = nh > 2 ? 1 : kWaves / nh, tail_head = wv / wph;
+  const int slot = lane >> 3, sub = lane & 7;
+  const int tail_first = max(sr.win_start - tail0, 0) >> 3, tail_chunks = (sr.n - tail0 + 7) >> 3;   // the window's
+  const int tail_begin = tail_first + part;
+  const bool tail_part = tail_begin < tail_chunks && a.window > 0;
+  auto load_tail = [&](int g, int c, bool selected, TailRows& t) {
+    const int r = min(8 * c + slot, sr.n - tail0 - 1);
+    const size_t at = (size_t)(head + g) * kD + sub * 8;
+    const size_t row = (((size_t)prob << shift) + r) * kD;
+    load_elems<8>((const T*)a.cache.k_tail + row + sub * 8, t.k);
+    load_elems<8>((const T*)a.cache.k_tail + row + kD / 2 + sub * 8, t.k + 8);
+    load_elems<16>((const T*)a.cache.v_tail + row + sub * 16, t.v);
+    if (selected) {
+      load_elems<8>(a.q_rot + at, t.q);
+      load_elems<8>(a.q_rot + at + kD / 2, t.q + 8);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        t.cs[e] = 1.f;
+        t.sn[e] = 0.f;
+      }
+    } else {
+      load_elems<8>((const T*)a.q + at, t.q);
+      load_elems<8>((const T*)a.q + at + kD / 2, t.q + 8);
+      const int delta = min(sr.n - 1 - tail0 - r, a.window - 1);
+      load8(a.cos_win + (size_t)delta * (kD / 2) + sub * 8, t.cs);
+      load8(a.sin_win + (size_t)delta * (kD / 2) + sub * 8, t.sn);
+    }
+  };
+  auto use_tail = [&](int c, bool selected, const TailRows& t, TailState& ts) {
+    const int r = 8 * c + slot;
+    const bool in = r < sr.n - tail0 && (selected ? (s_late[r >> 5] >> (r & 31) & 1u) != 0u : tail0 + r >= sr.win_start);
+    float dot = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      dot += t.q[e] * (t.k[e] * t.cs[e] + t.k[8 + e] * t.sn[e]);
+      dot += t.q[8 + e] * (t.k[8 + e] * t.cs[e] - t.k[e] * t.sn[e]);
+    }
+    dot = group8_fsum(dot);
+    const float lg = in ? dot * kLogit : -INFINITY;
+    const float mn = fmaxf(ts.m, lg), alpha = power(ts.m - mn), pr = power(lg - mn);
+    ts.l = ts.l * alpha + pr;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) ts.o[e] = ts.o[e] * alpha + (in ? pr * t.v[e] : 0.f);
+    ts.m = mn;
+  };
+  // The groups of 8 lanes are merged; again: with what the wave has stored for the head before.
+  auto store_tail = [&](int g, TailState& ts, bool again) {
+    const int to = GP == 8 ? g : wv;
+    float m = rows_max(fmaxf(ts.m, dpp<0x128>(ts.m)));
+    const float m_old = again ? s_tm[to] : kNone;
+    m = fmaxf(m, m_old);
+    const float f = power(ts.m - m), f_old = power(m_old - m);
+    float l = ts.l * f;
+    l = rows_sum(l + dpp<0x128>(l)) + (again ? s_tl[to] * f_old : 0.f);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      float o = ts.o[e] * f;
+      o = rows_sum(o + dpp<0x128>(o));
+      if (slot == 0) s_to[to][sub * 16 + e] = o + (again ? s_to[to][sub * 16 + e] * f_old : 0.f);
+    }
+    if (lane == 0) {
+      s_tm[to] = m;
+      s_tl[to] = l;
+    }
+  };
+
+  // A wave takes its pairs of the window, then those of the far rows, two of which are in flight at a time: a pair's keys and
+  // values are requested when those of the pair two before it have been used.  What does not depend on other loads comes first.
+  const int far_n = tail0 > 0 ? far_end - far_first : 0;
+  const bool has_win = win_first < n_win;
+  const int tail_c = tail_begin + a.parts * (wv % wph);
   WaveState st;
-  PairRows p;
+  PairRows pa, pc;
   Place far_place;
   st.m = kNone;
   st.l = 0.f;
 #pragma unroll
   for (int t = 0; t < 8; ++t) st.o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (win_first < n_win) {
+  auto load_far = [&](const uint32_t* rows, PairRows& p) {
+    load_keys(a.cache.k, rows, col, lrow * 32, 16, p);
+    load_values(a.cache.v, rows, col, lrow, p);
+  };
+  if (has_win) {
     float x[32];
     load_elems<16>((const T*)a.q + q_at + lrow * 16, x);
     load_elems<16>((const T*)a.q + q_at + kD / 2 + lrow * 16, x + 16);
     Place win_place = place_win(win_first);
-    if (has_far) far_place = place_far(far_first);
+    if (far_n > 0) far_place = place_far(fp[0], far_first);
     get_scales(win_place);
-    if (has_far) get_scales(far_place);
-    load_keys(a.cache.k, wp.row, col, lrow * 16, kD / 2, p);
-    load_values(a.cache.v, wp.row, col, lrow, p);
+    if (far_n > 0) get_scales(far_place);
+    load_keys(a.cache.k, wp.row, col, lrow * 16, kD / 2, pc);
+    load_values(a.cache.v, wp.row, col, lrow, pc);
+    if (far_n > 0) load_far(fp[0].row, pa);
     f16x8 qw[4];
     const float ww = query_terms(x, term, active, qw) * kLogit;
-    if (has_far) put_scales(pl, far_place);
+    if (far_n > 0) put_scales(fp[0], far_place);
 #pragma unroll 1
     for (int pair = win_first; pair < n_win; pair += kWaves) {
       f32x4 dot[2];
@@ -561,140 +644,102 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3, 3))
         float cs[16], sn[16];
         load_elems<16>(a.cos_win + (size_t)delta * (kD / 2) + lrow * 16, cs);
         load_elems<16>(a.sin_win + (size_t)delta * (kD / 2) + lrow * 16, sn);
-        const f32x4 acc = turned_dot<E4M3>(p.k[t], cs, sn, qw);
+        const f32x4 acc = turned_dot<E4M3>(pc.k[t], cs, sn, qw);
 #pragma unroll
         for (int i = 0; i < 4; ++i) dot[t][i] = head_sum<GP>(acc[i]) * ww;
       }
       put_scales(wp, win_place);
       float w[8];
       pair_weights(dot, wp, 0, lrow, st, w);
-      const bool more = pair + kWaves < n_win;
-      if (more) {
+      absorb_values<E4M3, GP, EXACT>(w, term, pc, st);
+      if (pair + kWaves < n_win) {
         win_place = place_win(pair + kWaves);
         get_scales(win_place);
-        load_keys(a.cache.k, wp.row, col, lrow * 16, kD / 2, p);
-      } else if (has_far) {
-        load_keys(a.cache.k, pl.row, col, lrow * 32, 16, p);
+        load_keys(a.cache.k, wp.row, col, lrow * 16, kD / 2, pc);
+        load_values(a.cache.v, wp.row, col, lrow, pc);
       }
-      absorb_values<E4M3, GP, EXACT>(w, term, p, st);
-      if (more || has_far) load_values(a.cache.v, more ? wp.row : pl.row, col, lrow, p);
     }
+    if (far_n > 1) load_far(fp[0].row + kPair, pc);
   }
-  if (has_far) {
+  if (far_n > 0) {
     FarQuery<E4M3, GP> fq;
     float x[32];
     load_elems<32>(a.q_rot + q_at + lrow * 32, x);
-    if (win_first >= n_win) {
-      far_place = place_far(far_first);
+    if (!has_win) {
+      far_place = place_far(fp[0], far_first);
       get_scales(far_place);
-      load_keys(a.cache.k, pl.row, col, lrow * 32, 16, p);
-      load_values(a.cache.v, pl.row, col, lrow, p);
-      put_scales(pl, far_place);
+      load_far(fp[0].row, pa);
+      if (far_n > 1) load_far(fp[0].row + kPair, pc);
+      put_scales(fp[0], far_place);
     }
-    unit = unit_of(far_row(far_first + 2));
+    if (far_n > 2) unit = unit_of(far_row(far_first + 2));
     fq.set(x, term, active);
-    int half = 0;
-#pragma unroll 1
-    for (int pair = far_first; pair < far_end; ++pair) {
+    auto use = [&](PairRows& p, const PairPlaces& pl, int first) {
       f32x4 dot[2];
       dot[0] = fq.dot(p.k[0]);
       dot[1] = fq.dot(p.k[1]);
       float w[8];
-      pair_weights(dot, pl, half * kPair, lrow, st, w);
-      const bool more = pair + 1 < far_end, again = half == 1 && more;
-      if (again) {
-        far_place = place_far(pair + 1);
-        get_scales(far_place);
-      }
-      const uint32_t* next = pl.row + (half ^ 1) * kPair;
-      if (more) load_keys(a.cache.k, next, col, lrow * 32, 16, p);
+      pair_weights(dot, pl, first, lrow, st, w);
       absorb_values<E4M3, GP, EXACT>(w, term, p, st);
-      if (more) load_values(a.cache.v, next, col, lrow, p);
-      if (again) {
-        put_scales(pl, far_place);
-        unit = unit_of(far_row(pair + 3));
+    };
+    int buf = 0;
+#pragma unroll 1
+    for (int i = 0; i < far_n; i += 2) {
+      const PairPlaces& pl = fp[buf];
+      PairPlaces& next = fp[buf ^ 1];
+      const bool more = i + 2 < far_n;
+      if (more) {
+        far_place = place_far(next, far_first + i + 2);
+        get_scales(far_place);
+        if (i + 4 < far_n) unit = unit_of(far_row(far_first + i + 4));
       }
-      half ^= 1;
+      use(pa, pl, 0);
+      if (more) load_far(next.row, pa);
+      if (i + 1 < far_n) use(pc, pl, kPair);
+      if (i + 3 < far_n) load_far(next.row + kPair, pc);
+      if (more) put_scales(next, far_place);
+      buf ^= 1;
+    }
+  }
+  if (tail_part) {
+#pragma unroll 1
+    for (int g = tail_head; g < (GP == 8 ? 8 : kWaves / wph); g += kWaves) {
+      TailState ts;
+      ts.m = kNone;
+      ts.l = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) ts.o[e] = 0.f;
+      if (g < nh) {
+#pragma unroll 1
+        for (int c = tail_c; c < tail_chunks; c += a.parts * wph) {
+          TailRows tr;
+          load_tail(g, c, false, tr);
+          use_tail(c, false, tr, ts);
+        }
+      }
+      store_tail(g, ts, false);
     }
   }
   __syncthreads();   // (the places are written again, with the outputs)
 
-  // The incomplete block: window rows of this part, and selected rows where the window is shorter than that block.  Up to
-  // four heads share out the waves, eight heads go to the four in turn.
-  const int wph = nh > 2 ? 1 : kWaves / nh;
-  const bool late = (s_late[0] | s_late[1] | s_late[2] | s_late[3]) != 0u, has_tail = late || w8 < w1;
-  if (has_tail) {
+  // Selected rows of the incomplete block (only where the window is shorter than that block).
+  const bool late = (s_late[0] | s_late[1] | s_late[2] | s_late[3]) != 0u, has_tail = late || tail_part;
+  if (late) {
 #pragma unroll 1
-    for (int g = wv / wph; g < (GP == 8 ? 8 : kWaves / wph); g += kWaves) {
-      const int at_slot = GP == 8 ? g : wv;
-      float m = kNone, l = 0.f, o[16];
+    for (int g = tail_head; g < (GP == 8 ? 8 : kWaves / wph); g += kWaves) {
+      if (g >= nh) continue;
+      TailState ts;
+      ts.m = kNone;
+      ts.l = 0.f;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) o[e] = 0.f;
-      const int slot = lane >> 3, sub = lane & 7;
-      if (g < nh) {
-        const T* kt = (const T*)a.cache.k_tail + ((size_t)prob << shift) * kD;
-        const T* vt = (const T*)a.cache.v_tail + ((size_t)prob << shift) * kD;
-        float qr[16], qv[16];   // elements 8 * sub + 0 .. 7 of either half
-        const size_t at = (size_t)(head + g) * kD;
-        load_elems<8>((const T*)a.q + at + sub * 8, qv);
-        load_elems<8>((const T*)a.q + at + kD / 2 + sub * 8, qv + 8);
-        load_elems<8>(a.q_rot + at + sub * 8, qr);
-        load_elems<8>(a.q_rot + at + kD / 2 + sub * 8, qr + 8);
-        const int r_first = late ? 0 : w8 - tail0, r_end = late ? sr.n - tail0 : w1 - tail0;
+      for (int e = 0; e < 16; ++e) ts.o[e] = 0.f;
 #pragma unroll 1
-        for (int r0 = r_first + (wv % wph) * 8; r0 < r_end; r0 += wph * 8) {
-          const int r = min(r0 + slot, r_end - 1), j = tail0 + r;
-          const bool win = j >= w8 && j < w1;
-          const bool in = r0 + slot < r_end && (win || (j < sr.win_start && (s_late[r >> 5] >> (r & 31) & 1u)));
-          float k[16], v[16], cs[8], sn[8];
-          load_elems<8>(kt + (size_t)r * kD + sub * 8, k);
-          load_elems<8>(kt + (size_t)r * kD + kD / 2 + sub * 8, k + 8);
-          load_elems<16>(vt + (size_t)r * kD + sub * 16, v);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) { cs[e] = 1.f; sn[e] = 0.f; }
-          if (win) {
-            const int delta = min(sr.n - 1 - j, a.window - 1);
-            load8(a.cos_win + (size_t)delta * (kD / 2) + sub * 8, cs);
-            load8(a.sin_win + (size_t)delta * (kD / 2) + sub * 8, sn);
-          }
-          float dot = 0.f;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float q0 = win ? qv[e] : qr[e], q1 = win ? qv[8 + e] : qr[8 + e];
-            dot += q0 * (k[e] * cs[e] + k[8 + e] * sn[e]);
-            dot += q1 * (k[8 + e] * cs[e] - k[e] * sn[e]);
-          }
-          dot = group8_fsum(dot);
-          const float lg = in ? dot * kLogit : -INFINITY;
-          const float mn = fmaxf(m, lg), alpha = power(m - mn), pr = power(lg - mn);
-          l = l * alpha + pr;
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[e] = o[e] * alpha + (in ? pr * v[e] : 0.f);
-          m = mn;
-        }
-        float mw = m;
-#pragma unroll
-        for (int off = 8; off < 64; off <<= 1) mw = fmaxf(mw, __shfl_xor(mw, off));
-        const float f = power(m - mw);
-        l *= f;
-#pragma unroll
-        for (int off = 8; off < 64; off <<= 1) l += __shfl_xor(l, off);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          o[e] *= f;
-#pragma unroll
-          for (int off = 8; off < 64; off <<= 1) o[e] += __shfl_xor(o[e], off);
-        }
-        m = mw;
+      for (int c = wv % wph; 8 * c < sr.n - tail0; c += wph) {
+        TailRows tr;
+        load_tail(g, c, true, tr);
+        use_tail(c, true, tr, ts);
       }
-      if (slot == 0) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s_to[at_slot][sub * 16 + e] = o[e];
-      }
-      if (lane == 0) {
-        s_tm[at_slot] = m;
-        s_tl[at_slot] = l;
-      }
+      store_tail(g, ts, tail_part);
     }
   }
 
