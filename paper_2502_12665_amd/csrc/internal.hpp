@@ -199,7 +199,8 @@ hipError_t launch_append(const a2ats_dims& d, const BlockCache& m, int kv_dtype,
 struct BlockTopkPlan {
   int total_blocks;     // of ctx_len tokens
   int chunk, chunks;    // blocks that a scoring workgroup takes, and workgroups of a (sequence, KV head)
-  size_t bytes;         // the scores
+  size_t off_largest;   // behind the scores: the chunks' largest magnitudes
+  size_t bytes;
 };
 BlockTopkPlan make_block_topk_plan(const a2ats_dims& d, int block, bool shared);
 hipError_t launch_block_topk(const a2ats_dims& d, const BlockCache& m, int kv_dtype, const void* q, const float* cos_b,
