@@ -410,6 +410,7 @@ class KvBlocks:
         self.block, self.kv_dtype, self.page_size, self.page_table = block, kv_dtype, page_size, page_table
         self.k, self.v, self.k_scale, self.v_scale, self.k_tail, self.v_tail, self.bounds = k, v, k_scale, v_scale, k_tail, v_tail, bounds
         self.device = (k if k is not None else bounds).device
+        self.device_index = (k if k is not None else bounds).get_device()
         for t in rows + (bounds, page_table):
             if t is not None and t.device != self.device:
                 raise ValueError("the tensors of a cache are on one device")
@@ -448,23 +449,23 @@ def _arg(cache: KvBlocks, t: Optional[torch.Tensor], name: str, dtype: torch.dty
     """Pointer of a tensor of a call on `cache`: of its device, its type and `numel` elements."""
     if t is None:
         return None
+    if t.dtype is dtype and t.get_device() == cache.device_index and t.numel() == numel and t.is_contiguous():
+        return t.data_ptr()
     if t.dtype != dtype:
         raise TypeError(f"{name} is {t.dtype}, not {dtype}")
     if t.device != cache.device:
         raise ValueError(f"{name} is on {t.device}, the cache on {cache.device}")
-    if t.numel() != numel or not t.is_contiguous():
-        raise ValueError(f"{name}: {numel} contiguous elements are wanted, not {tuple(t.shape)}")
-    return t.data_ptr()
+    raise ValueError(f"{name}: {numel} contiguous elements are wanted, not {tuple(t.shape)}")
 
 
 def _cache_stream(dims: Dims, cache: KvBlocks):
-    if (dims.batch, dims.n_kv_heads, dims.ctx_stride) != (cache.batch, cache.n_kv_heads, cache.ctx_stride):
+    if dims.batch != cache.batch or dims.n_kv_heads != cache.n_kv_heads or dims.ctx_stride != cache.ctx_stride:
         raise ValueError("dims are not those of the cache")
-    if cache.device.type != "cuda":
+    if cache.device_index < 0:
         raise ValueError(f"the cache is on {cache.device}")
-    if cache.device.index != torch.cuda.current_device():
+    if cache.device_index != torch.cuda.current_device():
         raise ValueError(f"the cache is on {cache.device}, the current device is {torch.cuda.current_device()}")
-    return torch.cuda.current_stream().cuda_stream
+    return torch._C._cuda_getCurrentRawStream(cache.device_index)   # current_stream() makes an object of it: 2.8 us
 
 
 def kv8_append(dims: Dims, cache: KvBlocks, k_new, v_new, n_new: int, seq_lens=None, new_lens=None):
