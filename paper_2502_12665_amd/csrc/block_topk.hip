@@ -85,8 +85,12 @@ struct TopkArgs {
   float* block_score;
   int32_t* token_idx;
   int32_t* token_count;
-  int32_t total_blocks, chunk, chunks, problems, ctx_len, window, n_sink, top_blocks, heads, group, shared;
+  int32_t total_blocks, chunks, problems, ctx_len, window, n_sink, top_blocks, heads, group, shared;
 };
+
+// Blocks of a sequence with n candidates that each of its workgroups scores: tiles of 16, shared out among as many as there are for
+// the longest sequence.
+__device__ __forceinline__ int chunk_blocks(int n, int chunks) { return ((n + chunks - 1) / chunks + 15) & ~15; }
 
 // The rotated elements of eight dimensions of a head and, with them, those of the other half: q R_b in float64, rounded once.
 template <typename T>
@@ -163,9 +167,9 @@ __global__ __launch_bounds__(kScoreThreads) void score_blocks_f64_kernel(TopkArg
     if (part == 0 && threadIdx.x < 16) store8(a.q_rot + ((size_t)prob * G + g) * kD + d0, r);
     eq.add(SHARED ? 0 : g, !SHARED || g == 0, r);
   }
-  const int end = min(last, first + (part + 1) * a.chunk);
+  const int chunk = chunk_blocks(last - first, a.chunks), begin = first + part * chunk, end = min(last, begin + chunk);
   const float* bounds = (const float*)a.cache.bounds;
-  for (int c0 = first + part * a.chunk + group; c0 - (group & 3) < end; c0 += U * GROUPS) {
+  for (int c0 = begin + group; c0 - (group & 3) < end; c0 += U * GROUPS) {
     float lo[U][8], hi[U][8];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -262,21 +266,34 @@ __device__ __forceinline__ void make_query_step(const TopkArgs& a, int s, size_t
   load8(a.sin_b + t, sn);
 #pragma unroll
   for (int e = 0; e < 8; ++e) pos[e] = neg[e] = 0.f;
-#pragma unroll 2
-  for (int g = 0; g < n; ++g) {
-    const int h = sum ? g : min(col % GP, heads - 1);
-    const uint16_t* row = (const uint16_t*)a.q + (head0 + h) * kD;
-    float own[8], other[8], r[8];
-    load8(row + half * (kD / 2) + t, own);
-    load8(row + (half ^ 1) * (kD / 2) + t, other);
+  constexpr int AHEAD = 4;   // heads whose loads are requested together
+  for (int g0 = 0; g0 < n; g0 += AHEAD) {
+    uint4 own_raw[AHEAD], other_raw[AHEAD];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const double x = (double)own[e] * cs[e], y = (double)other[e] * sn[e];
-      r[e] = (float)(half ? x + y : x - y);
-      pos[e] += active ? fmaxf(r[e], 0.f) : 0.f;
-      neg[e] += active ? fminf(r[e], 0.f) : 0.f;
+    for (int k = 0; k < AHEAD; ++k) {
+      const int h = sum ? min(g0 + k, n - 1) : min(col % GP, heads - 1);
+      if (k == 0 || sum) {
+        const uint16_t* row = (const uint16_t*)a.q + (head0 + h) * kD + t;
+        own_raw[k] = *(const uint4*)(row + half * (kD / 2));
+        other_raw[k] = *(const uint4*)(row + (half ^ 1) * (kD / 2));
+      }
     }
-    if (write && (sum ? col == 0 : col < heads)) store8(a.q_rot + (head0 + h) * kD + half * (kD / 2) + t, r);
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      if (g0 + k >= n) continue;
+      const int h = sum ? g0 + k : min(col % GP, heads - 1);
+      float own[8], other[8], r[8];
+      widen8(own_raw[k], own);
+      widen8(other_raw[k], other);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const double x = (double)own[e] * cs[e], y = (double)other[e] * sn[e];
+        r[e] = (float)(half ? x + y : x - y);
+        pos[e] += active ? fmaxf(r[e], 0.f) : 0.f;
+        neg[e] += active ? fminf(r[e], 0.f) : 0.f;
+      }
+      if (write && (sum ? col == 0 : col < heads)) store8(a.q_rot + (head0 + h) * kD + half * (kD / 2) + t, r);
+    }
   }
 #pragma unroll
   for (int k = 0; k < MatrixQuery<GP>::SETS; ++k) {
@@ -307,7 +324,7 @@ __global__ __launch_bounds__(kScoreThreads) void score_blocks_kernel(TopkArgs a)
   const SeqRange sr = seq_range(a.ctx_len, a.seq_lens, b, a.window, a.n_sink, 0);
   int first, last;
   candidate_blocks(sr, a.cache.shift, first, last);
-  const int c0 = first + part * a.chunk, end = min(last, c0 + a.chunk);
+  const int chunk = chunk_blocks(last - first, a.chunks), c0 = first + part * chunk, end = min(last, c0 + chunk);
   if (c0 >= end && part > 0) return;   // (uniform; the first part writes the rotated queries)
   const uint16_t* bounds = (const uint16_t*)a.cache.bounds;
   // Two tiles of 16 blocks are in flight.
@@ -412,9 +429,10 @@ __global__ __launch_bounds__(kPickThreads) void pick_blocks_kernel(TopkArgs a) {
   }
   if constexpr (MATRIX) {
     __syncthreads();
+    const int chunk = chunk_blocks(n, a.chunks);
     float big = 0.f;
     for (int i = tid; i < a.chunks; i += NT)
-      if (i * a.chunk < n) big = fmaxf(big, a.largest[((size_t)b * a.cache.n_kv_heads + kv) * a.chunks + i]);   // (as bits: not negative)
+      if (i * chunk < n) big = fmaxf(big, a.largest[((size_t)b * a.cache.n_kv_heads + kv) * a.chunks + i]);   // (as bits: not negative)
     const uint32_t bits = wave_max_to_last_lane(__float_as_uint(big));
     if (lane == 63 && wv < (a.chunks + 63) / 64) atomicMax(&s_big, bits);
   }
@@ -668,9 +686,7 @@ BlockTopkPlan make_block_topk_plan(const a2ats_dims& d, int block, bool shared) 
   // Two workgroups a CU, each with 64 blocks at least (a tile for every wave).
   long chunks = problems > 0 ? (512 + problems - 1) / problems : 1;
   chunks = std::max(1l, std::min(chunks, (long)p.total_blocks / 64));
-  p.chunk = std::max(1, (int)((p.total_blocks + chunks - 1) / chunks));
-  p.chunk = (p.chunk + 15) / 16 * 16;
-  p.chunks = std::max(1, (p.total_blocks + p.chunk - 1) / p.chunk);
+  p.chunks = (int)chunks;
   const size_t scores = (size_t)d.batch * (shared ? d.n_kv_heads : d.n_q_heads) * p.total_blocks * sizeof(float);
   p.off_largest = (scores + 255) / 256 * 256;
   p.bytes = p.off_largest + (size_t)problems * p.chunks * sizeof(float);
@@ -715,7 +731,6 @@ hipError_t launch_block_topk(const a2ats_dims& d, const BlockCache& m, int kv_dt
   a.token_idx = token_idx;
   a.token_count = token_count;
   a.total_blocks = p.total_blocks;
-  a.chunk = p.chunk;
   a.chunks = p.chunks;
   a.problems = d.batch * d.n_kv_heads;
   a.ctx_len = d.ctx_len;

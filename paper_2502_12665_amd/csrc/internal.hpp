@@ -198,7 +198,7 @@ hipError_t launch_append(const a2ats_dims& d, const BlockCache& m, int kv_dtype,
                          const void* v_new, int n_new, const int32_t* seq_lens, const int32_t* new_lens, hipStream_t stream);
 struct BlockTopkPlan {
   int total_blocks;     // of ctx_len tokens
-  int chunk, chunks;    // blocks that a scoring workgroup takes, and workgroups of a (sequence, KV head)
+  int chunks;           // workgroups that score the blocks of a (sequence, KV head)
   size_t off_largest;   // behind the scores: the chunks' largest magnitudes
   size_t bytes;
 };

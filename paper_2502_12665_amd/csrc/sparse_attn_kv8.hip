@@ -825,13 +825,23 @@ __global__ __launch_bounds__(kD) void attn_kv8_merge_kernel(const float* __restr
 
 }  // namespace
 
+// Parts: a second launch (2.5 us) and as many more first requests to wait for, against rows that wait for each other.  From all
+// counts of parts up to 32 of 2 to 896 problems with 160 to 2304 rows (bfloat16, int8, selections of one head and shared by four), us
+// with one part -> with the parts taken:
+//   - a workgroup for every CU where there are few problems: 4 problems, 576 rows 10.4 -> 8.4 (8 parts), 2304 rows 27.0 -> 9.9
+//     (12); 32 problems, 1152 rows 17.1 -> 9.7 (8); 64 problems, 576 rows 11.2 -> 9.7 (4); but 160 rows of any number of problems
+//     are faster in one part (6.5 -> 8.1 for two);
+//   - up to 128 problems, 1152 rows 17.9 -> 15.2 (2), 576 rows would be 11.9 -> 12.6; 2304 rows 31.2 -> 20.6 (4);
+//   - many rows of up to 511 problems in two: 256 problems, 2304 rows 39.1 -> 37.0, 384 problems 56.5 -> 53.0, but 512 problems
+//     62.4 -> 66.2, and 1152 rows of 256 problems 20.1 -> 20.7.
 Kv8Plan make_kv8_plan(const a2ats_dims& d, long sel_rows, int window, bool shared) {
   Kv8Plan p;
   const long problems = (long)d.batch * (shared ? d.n_kv_heads : d.n_q_heads);
   const long rows = std::min<long>(sel_rows, d.ctx_len) + std::min(window, d.ctx_len);
-  // Two workgroups a CU, each with a pair of tiles at least for every wave.
-  long parts = problems > 0 ? (512 + problems - 1) / problems : 1;
-  parts = std::max(1l, std::min(std::min(parts, rows / (kWaves * kPair)), 32l));
+  long parts = 1;
+  if (problems <= 64) parts = rows < 350 ? 1 : std::min(std::min(problems > 0 ? 256 / problems : 1, rows / 72), 12l);
+  else if (problems <= 128) parts = rows >= 1600 ? 4 : (rows >= 800 ? 2 : 1);
+  else if (problems < 512) parts = rows >= 1600 ? 2 : 1;
   p.parts = (int)parts;
   p.bytes = parts > 1 ? (size_t)d.batch * d.n_q_heads * parts * (kD + 2) * sizeof(float) : 0;
   return p;
