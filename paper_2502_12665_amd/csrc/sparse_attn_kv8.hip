@@ -8,9 +8,9 @@
 // has to stay below its bytes.  Both products are on the matrix cores, also for one head, with the 16 columns of a tile used for
 // the precision of the float32 operand:
 //   - keys (A, 16 rows x 128) times queries (B).  A column is (head, term): int8 keys go into v_mfma_i32_16x16x64_i8 as they
-//     come from memory, the query as three signed digits to the base 256 of q * 2^(22 - e), |q| < 2^e, so that a logit is an
-//     exact integer sum; e4m3 keys become float16 (exact) and the query two float16 terms.  The terms of a head are added
-//     across the columns of a lane row.
+//     come from memory, the query as four signed digits to the base 256 of q * 2^(30 - e), |q| < 2^e, so that each digit's product
+//     is an exact integer; e4m3 keys become float16 (exact) and the query three float16 terms (eight heads: two, 22 bits).  The
+//     terms of a head are added across the columns of a lane row.
 //   - values (A, 16 dimensions x 32 rows) times weights (B).  Logits leave the first product with a head in each column and
 //     four rows of each of two tiles in each lane, which is the B operand of the second as it stands: no exchange between lanes.
 //     Weights are split into bfloat16 terms by truncation, again a column each: the range of float32 stays (v_scale is in the
@@ -46,11 +46,12 @@ template <int CTRL>
 __device__ __forceinline__ float dpp(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
 }
-// Sum over the columns of a head, c, c + GP, .. of 16, in every lane.
+// Sum over the columns of a head, c, c + GP, .. of 16: the same bits in each of them (the terms of a weight, a column each, are
+// only its terms if they are those of one number), as the first sums repeat after eight columns.
 template <int GP>
 __device__ __forceinline__ float head_sum(float v) {
-  if (GP == 4) v += dpp<0x124>(v);   // row_ror:4
   v += dpp<0x128>(v);                // row_ror:8
+  if (GP == 4) v += dpp<0x124>(v);   // row_ror:4
   return v;
 }
 // Over the four lane rows, in every lane.
@@ -83,6 +84,10 @@ __device__ __forceinline__ uint32_t upper_halves(float a, float b) {
   return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
 }
 __device__ __forceinline__ uint32_t f16_bits(f16x2 v) { return __builtin_bit_cast(uint32_t, v); }
+__device__ __forceinline__ f16x2 f16_pair(float a, float b) {
+  typedef __attribute__((ext_vector_type(2))) float f32x2;
+  return __builtin_convertvector((f32x2){a, b}, f16x2);   // (to the nearest)
+}
 
 template <int N>
 __device__ __forceinline__ void load_elems(const float* p, float* x) {
@@ -105,6 +110,12 @@ __device__ __forceinline__ void load_elems(const uint16_t* p, float* x) {
 __device__ __forceinline__ void store_elem(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_elem(uint16_t* p, float v) { *p = f32_to_bf16(v); }
 
+// Logits times log2 e, from the queries on: the rounding is each element's own, and the factors behind are powers of two.
+__device__ __forceinline__ void to_logits(float (&x)[32]) {
+#pragma unroll
+  for (int i = 0; i < 32; ++i) x[i] *= kLogit;
+}
+
 // The least e >= -100 with |x| < 2^e for all x of a head's row (32 elements in this lane, the others in the lane rows);
 // ok: all are finite.
 __device__ __forceinline__ int row_exponent(const float (&x)[32], bool& ok) {
@@ -119,20 +130,24 @@ __device__ __forceinline__ int row_exponent(const float (&x)[32], bool& ok) {
   return max((int)(big >> 23) - 126, -100);
 }
 
-// A query as float16 terms, for the columns of the first two: x = 2^e (hi + lo), to 2^-22 of 2^e.  Returns 2^e.
+// A query as float16 terms, for the columns of the first three (eight heads: two): x = 2^(e - 8) (t0 + t1 + t2), all bits of it
+// that are above 2^-24 (2^-14 of the least term) of 2^e.  Returns 2^(e - 8).
+template <int GP>
 __device__ __forceinline__ float query_terms(const float (&x)[32], int term, bool active, f16x8 (&q)[4]) {
   bool ok;
   const int e = row_exponent(x, ok);
-  const float down = ldexpf(active && term < 2 ? 1.f : 0.f, -e);   // (2^-128 is a subnormal number, and exact)
-  const float less = term == 1 ? 1.f : 0.f;
+  const float down = ldexpf(active && term < 3 ? 1.f : 0.f, 8 - e);
+  const float less1 = term >= 1 ? 1.f : 0.f, less2 = term >= 2 ? 1.f : 0.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float y = x[8 * i + j] * down;
-      q[i][j] = (_Float16)(y - less * (float)(_Float16)y);
+      float y = x[8 * i + j] * down;
+      y -= less1 * (float)(_Float16)y;
+      if (GP == 4) y -= less2 * (float)(_Float16)y;
+      q[i][j] = (_Float16)y;
     }
-  return ok ? ldexpf(1.f, e) : __uint_as_float(0x7fc00000u);
+  return ok ? ldexpf(1.f, e - 8) : __uint_as_float(0x7fc00000u);
 }
 
 struct AttnArgs {
@@ -299,40 +314,39 @@ __device__ __forceinline__ void absorb_values(const float (&weight)[8], int term
   }
 }
 
-// The queries of far rows as the second operand: int8 caches, three digits of eight bits; e4m3, two float16 terms.
+// The queries of far rows as the second operand: int8 caches, four digits of eight bits; e4m3, float16 terms.
 template <bool E4M3, int GP>
 struct FarQuery {
-  i32x4 d[E4M3 ? 1 : 2], d2[GP == 8 && !E4M3 ? 2 : 1];   // (eight heads: the third digit by itself)
+  i32x4 d[E4M3 ? 1 : 2], d2[GP == 8 && !E4M3 ? 2 : 1];   // (eight heads: the third and the fourth digit)
   f16x8 f[E4M3 ? 4 : 1];
   float cw, cw2;   // what a column's product is worth
   // Elements 32 * lane row + 0 .. 31 of the column's head.
   __device__ __forceinline__ void set(const float (&x)[32], int term, bool active) {
     cw2 = 0.f;
     if constexpr (E4M3) {
-      cw = query_terms(x, term, active, f) * kLogit;
+      cw = query_terms<GP>(x, term, active, f);
     } else {
       bool ok;
       const int e = row_exponent(x, ok);
-      // v = rint(x 2^(22 - e)) is the low bits of x 2^(22 - e) + 3 * 2^22; v = (d0 256 + d1) 256 + d2 with signed digits:
-      // d2 = v, d1 = (v + 0x80) >> 8, d0 = (v + 0x8080) >> 16, the low 8 bits of each.
-      const float up = ldexpf(active ? 1.f : 0.f, 22 - e);
-      const uint32_t magic = 0x4b400000u, shift = term == 0 ? 16u : (term == 1 ? 8u : 0u);
-      const uint32_t bias = (term == 0 ? 0x8080u : (term == 1 ? 0x80u : 0u)) - magic;
-      const uint32_t mask = term == 3 ? 0u : 0xffu, mask2 = term == 0 ? 0xffu : 0u;
+      // v = x 2^(30 - e), a whole number but for what is below 2^-30 of 2^e; v = ((d0 256 + d1) 256 + d2) 256 + d3 with signed
+      // digits: d3 = v, d2 = (v + 0x80) >> 8, d1 = (v + 0x8080) >> 16, d0 = (v + 0x808080) >> 24, the low 8 bits of each.
+      const float up = ldexpf(active ? 1.f : 0.f, 30 - e);
+      const uint32_t shift = 24u - 8u * (uint32_t)term, shift2 = GP == 8 ? 8u - 8u * (uint32_t)term : 0u;
+      const uint32_t bias = 0x808080u & ((1u << shift) - 1u), bias2 = 0x80u & ((1u << shift2) - 1u);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         uint32_t w = 0u, w2 = 0u;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint32_t v = __float_as_uint(__builtin_fmaf(x[4 * i + j], up, 12582912.f));
-          w |= (((v + bias) >> shift) & mask) << (8 * j);
-          if (GP == 8) w2 |= (v & mask2) << (8 * j);
+          const uint32_t v = (uint32_t)(int)(x[4 * i + j] * up);
+          w |= (((v + bias) >> shift) & 0xffu) << (8 * j);
+          if (GP == 8) w2 |= (((v + bias2) >> shift2) & 0xffu) << (8 * j);
         }
         d[i / 4][i % 4] = (int)w;
         if constexpr (GP == 8) d2[i / 4][i % 4] = (int)w2;
       }
-      cw = ok ? ldexpf(kLogit, e - 22 + (int)shift) : __uint_as_float(0x7fc00000u);
-      if (GP == 8) cw2 = ldexpf(kLogit, e - 22);
+      cw = ok ? ldexpf(1.f, e - 30 + (int)shift) : __uint_as_float(0x7fc00000u);
+      if (GP == 8) cw2 = ldexpf(1.f, e - 30 + (int)shift2);
     }
   }
   // Products of a tile's keys (32 elements of row `column`) with the queries: rows 4 * lane row + i.
@@ -399,10 +413,9 @@ __device__ __forceinline__ f32x4 turned_dot(const uint4 (&k)[2], const float (&c
       uint32_t hi[4], lo[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const auto h = __builtin_amdgcn_cvt_pkrtz(x[2 * j], x[2 * j + 1]);
-        const auto r = __builtin_amdgcn_cvt_pkrtz(x[2 * j] - (float)h[0], x[2 * j + 1] - (float)h[1]);
-        hi[j] = __builtin_bit_cast(uint32_t, h);
-        lo[j] = __builtin_bit_cast(uint32_t, r);
+        const f16x2 h = f16_pair(x[2 * j], x[2 * j + 1]);
+        hi[j] = f16_bits(h);
+        lo[j] = f16_bits(f16_pair(x[2 * j] - (float)h[0], x[2 * j + 1] - (float)h[1]));
       }
       acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, make_uint4(hi[0], hi[1], hi[2], hi[3])), qt, acc, 0, 0, 0);
       acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, make_uint4(lo[0], lo[1], lo[2], lo[3])), qt, acc, 0, 0, 0);
@@ -633,7 +646,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     load_values(a.cache.v, wp.row, col, lrow, pc);
     if (far_n > 0) load_far(fp[0].row, pa);
     f16x8 qw[4];
-    const float ww = query_terms(x, term, active, qw) * kLogit;
+    to_logits(x);
+    const float ww = query_terms<GP>(x, term, active, qw);
     if (far_n > 0) put_scales(fp[0], far_place);
 #pragma unroll 1
     for (int pair = win_first; pair < n_win; pair += kWaves) {
@@ -673,6 +687,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       put_scales(fp[0], far_place);
     }
     if (far_n > 2) unit = unit_of(far_row(far_first + 2));
+    to_logits(x);
     fq.set(x, term, active);
     auto use = [&](PairRows& p, const PairPlaces& pl, int first) {
       f32x4 dot[2];

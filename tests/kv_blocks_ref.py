@@ -97,7 +97,7 @@ def tokens_of(blocks, n, blk, window, n_sink):
     return [j for c in blocks for j in range(c * blk, (c + 1) * blk) if lo <= j < hi]
 
 
-def attend(q, q_rot, k, v, n, positions, window, n_sink, cos_win, sin_win):
+def attend(q, q_rot, k, v, n, positions, window, n_sink, cos_win, sin_win, roundings=2 * (128 + 8)):
     """One head.  k, v [n, D] float64; positions: selected candidates.  -> (out [D], error scale [D]): the second is what
     float32 arithmetic of any order may be off by, see `bound`."""
     lo, hi = candidates(n, window, n_sink)
@@ -112,15 +112,15 @@ def attend(q, q_rot, k, v, n, positions, window, n_sink, cos_win, sin_win):
     rows, vals = k[at], v[at]
     logit = (heads * rows).sum(-1) / math.sqrt(D)
     p = torch.softmax(logit, 0)
-    return p @ vals, bound(heads, rows, p, vals)
+    return p @ vals, bound(heads, rows, p, vals, roundings)
 
 
-def bound(heads, rows, p, vals):
+def bound(heads, rows, p, vals, roundings):
     """float32 with u = 2^-24.  A logit is a sum of 128 products of factors with at most three roundings each (a key turned by its
     window position: two products and a sum, 4 u of both halves; scales: 2 u): off by at most (128 + 8) u sum |q k| / sqrt(128),
     where a turned row's |q k| is at most |q| |k|' with both halves: twice as much covers it.  A weight has that in its
     exponent, and 8 u for the exponential and the rescalings (each exp2 argument of size up to 64: 64 u more); sums of weights
     and of p v over the rows add (rows + 16) u.  Numerator and denominator: twice."""
     u = 2.0 ** -24
-    d = (2 * (128 + 8) * u * (heads.abs() * rows.abs()).sum(-1) / math.sqrt(D)).max() + 72 * u + (len(p) + 16) * u
+    d = (roundings * u * (heads.abs() * rows.abs()).sum(-1) / math.sqrt(D)).max() + 72 * u + (len(p) + 16) * u
     return 2 * d * (p @ vals.abs())

@@ -419,6 +419,25 @@ def test_attention_shared_out_or_not(batch, heads, kv_heads, n, n_sel, shared):
     assert torch.equal(got[0], again[0])                    # the workspace's contents do not matter, nor the run
 
 
+@pytest.mark.parametrize("shared, G", [(False, 4), (True, 3), (True, 6)])
+def test_products_of_int8_keys_are_exact(shared, G):
+    """Products of int8 keys with a query's digits are whole numbers: a logit is off by the query's own rounding (one, of each element), the sums of its
+    terms (at most 4 roundings of at most sum |q k| each), the scale and the difference to the maximum: 8 u, not 272, of sum |q k| / sqrt(128).
+    Many heads of few rows, so that one weight whose terms do not belong together would show."""
+    c = Case([96] * 40, 2 * G, 2, 32, "i8", "f32", seed=75, bounds=False)
+    c.append(c.lens)
+    sel = draw_sel(c, 1, shared, 60, 0, 0, 76)
+    got, q_rot, cos_w, sin_w = run_attend(c, sel, 1, shared, 0, 0)
+    for b in range(c.batch):
+        for h in range(c.heads):
+            kv = h // c.G
+            s = c.seq(b, kv) if h % c.G == 0 else s
+            want, off = R.attend(c.q[b, h].double(), q_rot[b, h].double(), s.rows["k"], s.rows["v"], 96, sel[b][kv if shared else h], 0, 0,
+                                 cos_w, sin_w, roundings=8)
+            err = (got[b, h].double() - want).abs()
+            assert (err <= off * (1 + 2.0 ** -24) + 2.0 ** -24 * want.abs()).all(), (b, h, float(err.max()), float(off.max()))
+
+
 @pytest.mark.parametrize("window", [0, 1, 700, 5000])
 def test_attention_of_the_window_alone(window):
     c = Case([700, 3, 64, 0], 4, 4, 64, "e4m3", "bf16", seed=70, bounds=False)
