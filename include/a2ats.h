@@ -476,8 +476,8 @@ int a2ats_key_bounds(const a2ats_dims* dims, const a2ats_kv_blocks* blocks, cons
  * offset (section 4.1), q~ = q R_b, so that for the bounds lo, hi of a block's pre-RoPE keys
  *     q~ . k_j  <=  score = sum_d max(q~_d lo_d, q~_d hi_d)    for every token j of the block.
  * Candidates are the blocks that hold a candidate token, [sink_end, n - window) as in a2ats_score_topk; the top_blocks
- * (<= 4096) with the highest scores are selected, equal scores to the lower block.  Scores are float64 sums rounded once to float32; a score that
- * is not a number counts as infinite.
+ * (<= 4096) with the highest scores are selected, equal scores to the lower block.  Scores are float64 sums rounded once to float32; one whose query
+ * or bounds are not all finite is infinite.
  *   shared 0: for each query head, H = Hq;  otherwise: for each KV head, H = Hkv, score = the sum over its G query heads
  *   q           [dev, kv_dtype B*Hq*D], cos_b / sin_b as in a2ats_build_lut, q_rot [dev, out, f32 B*Hq*D] as there (16-byte aligned)
  *   block_idx   [dev, out, int32 B*H*top_blocks]  ascending, slots past block_count are -1

@@ -78,7 +78,7 @@ struct TopkArgs {
   const float* sin_b;
   float* q_rot;
   float* scores;        // [head][total_blocks]
-  float* largest;       // [sequence, KV head][chunk]: of the magnitudes of a chunk's bounds
+  uint32_t* largest;    // [sequence, KV head][chunk]: of the magnitudes of a chunk's bounds, a float's bits
   const int32_t* seq_lens;
   int32_t* block_idx;
   int32_t* block_count;
@@ -372,7 +372,7 @@ __global__ __launch_bounds__(kScoreThreads) void score_blocks_kernel(TopkArgs a)
     uint32_t m = s_big[0];
 #pragma unroll
     for (int w = 1; w < NW; ++w) m = max(m, s_big[w]);
-    a.largest[(size_t)prob * a.chunks + part] = __uint_as_float(m << 16);
+    a.largest[(size_t)prob * a.chunks + part] = m << 16;
   }
 }
 
@@ -430,11 +430,11 @@ __global__ __launch_bounds__(kPickThreads) void pick_blocks_kernel(TopkArgs a) {
   if constexpr (MATRIX) {
     __syncthreads();
     const int chunk = chunk_blocks(n, a.chunks);
-    float big = 0.f;
+    uint32_t big = 0u;   // (as bits: what is not a number is the largest)
     for (int i = tid; i < a.chunks; i += NT)
-      if (i * chunk < n) big = fmaxf(big, a.largest[((size_t)b * a.cache.n_kv_heads + kv) * a.chunks + i]);   // (as bits: not negative)
-    const uint32_t bits = wave_max_to_last_lane(__float_as_uint(big));
-    if (lane == 63 && wv < (a.chunks + 63) / 64) atomicMax(&s_big, bits);
+      if (i * chunk < n) big = max(big, a.largest[((size_t)b * a.cache.n_kv_heads + kv) * a.chunks + i]);
+    big = wave_max_to_last_lane(big);
+    if (lane == 63 && wv < (a.chunks + 63) / 64) atomicMax(&s_big, big);
   }
   __syncthreads();
 
@@ -689,7 +689,7 @@ BlockTopkPlan make_block_topk_plan(const a2ats_dims& d, int block, bool shared) 
   p.chunks = (int)chunks;
   const size_t scores = (size_t)d.batch * (shared ? d.n_kv_heads : d.n_q_heads) * p.total_blocks * sizeof(float);
   p.off_largest = (scores + 255) / 256 * 256;
-  p.bytes = p.off_largest + (size_t)problems * p.chunks * sizeof(float);
+  p.bytes = p.off_largest + (size_t)problems * p.chunks * sizeof(uint32_t);
   return p;
 }
 
@@ -723,7 +723,7 @@ hipError_t launch_block_topk(const a2ats_dims& d, const BlockCache& m, int kv_dt
   a.sin_b = sin_b;
   a.q_rot = q_rot;
   a.scores = (float*)ws;
-  a.largest = (float*)((char*)ws + p.off_largest);
+  a.largest = (uint32_t*)((char*)ws + p.off_largest);
   a.seq_lens = seq_lens;
   a.block_idx = block_idx;
   a.block_count = block_count;

@@ -325,6 +325,39 @@ def test_select_survives_what_is_not_finite():
     assert idx.cpu().tolist() == [[[0, 1, 2, 3]] * 2]
 
 
+@pytest.mark.parametrize("wrong", [math.nan, math.inf, -math.inf, None])
+def test_select_of_scores_that_cancel(wrong):
+    """Scores of 16 and a little that are what large terms leave: 4096 + a - 4080 - a + t with |a| < 2^-7 (lost in part beside 4096) and
+    |t| < 2^-12.  A block whose bounds are not finite does not change how the others are told apart."""
+    blk, n = 16, 120
+    dims = dims_of(1, 1, 1, n * blk, n * blk)
+    g = gen(36)
+    q, key = torch.zeros(1, 1, D), torch.zeros(n, D)
+    q[..., [0, 1, 40, 70, 71]] = 1.0
+    key[:, 0], key[:, 40] = 4096.0, -4080.0
+    key[:, 1] = ((torch.rand(n, generator=g) - 0.5) * 2.0 ** -6).bfloat16().float()
+    key[:, 70] = -key[:, 1]
+    key[:, 71] = ((torch.rand(n, generator=g) - 0.5) * 2.0 ** -11).bfloat16().float()
+    key[0, 40] = -4088.0 if wrong is None else -4096.0
+    key[0, 70] = -key[0, 1] + (0.0 if wrong is None else 8.0)
+    score = key.double().sum(-1).float()                   # (exact in float64)
+    if wrong is not None:
+        key[77, 5] = wrong
+        q[..., 5] = 2.0 ** -20
+        score[77] = math.inf
+    c = Case.__new__(Case)
+    c.batch, c.heads, c.kv_heads, c.G, c.blk, c.page, c.dims, c.have = 1, 1, 1, 1, blk, 0, dims, [n * blk]
+    c.cache = B.KvBlocks(dims, blk, torch.bfloat16, bounds=key.bfloat16()[None, None, :, None].expand(1, 1, n, 2, D).contiguous().cuda())
+    order = sorted(range(n), key=lambda i: (-float(score[i]), i))
+    one, zero = torch.ones(64, device="cuda"), torch.zeros(64, device="cuda")
+    for top in (1, 20, 60, 90, 119):
+        idx = torch.full((1, 1, top), -9, dtype=torch.int32, device="cuda")
+        cnt = torch.zeros(1, 1, dtype=torch.int32, device="cuda")
+        ws = torch.empty(B.workspace_bytes(dims, B.OP_BLOCK_TOPK), dtype=torch.uint8, device="cuda")
+        B.block_topk(dims, c.cache, q.bfloat16().cuda(), one, zero, torch.empty(1, 1, D, device="cuda"), False, top, 0, 0, None, idx, cnt, ws=ws)
+        assert idx.cpu()[0, 0].tolist() == sorted(order[:top]), top
+
+
 # ---------------------------------------------------------------------------------------------- attention
 
 def run_attend(c, sel, size, shared, window, n_sink, ws_fill=0xFF, q_rot=None):
