@@ -484,7 +484,7 @@ int a2ats_key_bounds(const a2ats_dims* dims, const a2ats_kv_blocks* blocks, cons
  *   block_count [dev, out, int32 B*H]             min(top_blocks, candidates)
  *   block_score [dev, out, nullable, f32 B*H*top_blocks]  (0 past block_count)
  *   token_idx   [dev, out, nullable, int32 B*H*top_blocks*block] the candidate tokens of the selected blocks, ascending, then -1,
- *   token_count [dev, out, nullable, int32 B*H]   and their number (both or neither): with
+ *   token_count [dev, out, nullable, int32 B*H]   and their number (both or, if top_blocks > 0, neither): with
  *               top_k = top_blocks * block these are the topk_idx / topk_count of a2ats_sparse_attn (shared:
  *               a2ats_sparse_attn_shared) and its other forms.
  * Of `blocks` only bounds, block, kv_dtype, page_table and page_size are read.
@@ -503,7 +503,8 @@ int a2ats_block_topk(const a2ats_dims* dims, const a2ats_kv_blocks* blocks, cons
  *   shared 0: of each query head, H = Hq;  otherwise of each KV head, H = Hkv, attended by its G heads.
  * Indices may be in any order but not repeat; what is not a candidate, [sink_end, n - window), is not attended.
  * Rows of complete blocks are code * scale, those of the incomplete block are in the tails.  float32 accumulation; out
- * [dev, out, kv_dtype B*Hq*D] is rounded once (zeros where nothing is attended).  q, q_rot, cos_win, sin_win as in
+ * [dev, out, kv_dtype B*Hq*D] is rounded once (zeros where nothing is attended, else NaN for a head whose query is not
+ * finite).  q, q_rot, cos_win, sin_win as in
  * a2ats_sparse_attn (all 16-byte aligned); `bounds` is not read.
  * Workspace: a2ats_workspace_bytes(dims, A2ATS_OP_ATTN_KV8, n_sel * sel_size, window).
  */

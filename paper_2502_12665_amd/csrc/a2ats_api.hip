@@ -55,6 +55,10 @@ int log2_of(int v) {
   while ((1 << s) < v) ++s;
   return s;
 }
+// Whether a launch of `parts` workgroups for each sequence and head has fewer than 2^32 threads, all that HIP takes.
+bool launchable(const a2ats_dims& d, int64_t heads, int64_t parts, int64_t threads) {
+  return (double)d.batch * (double)heads * (double)parts * (double)threads < 4294967296.0;
+}
 int check_blocks(const a2ats_dims& d, const a2ats_kv_blocks* c, bool rows, bool bounds, a2ats::BlockCache* m) {
   if (!c) return A2ATS_ERR_INVALID_ARG;
   if (c->block < kLeastBlock || (c->block & (c->block - 1))) return A2ATS_ERR_INVALID_ARG;
@@ -689,8 +693,9 @@ static int append_impl(const a2ats_dims* d, const a2ats_kv_blocks* blocks, bool 
   rc = check_blocks(*d, blocks, rows, !rows, &m);
   if (rc != A2ATS_OK) return rc;
   if (n_new < 0 || n_new > d->ctx_len) return A2ATS_ERR_INVALID_ARG;
+  if (n_new == 0) return A2ATS_OK;
   if (!k_new || misaligned16(k_new) || (rows && (!v_new || misaligned16(v_new)))) return A2ATS_ERR_INVALID_ARG;
-  if ((int64_t)d->batch * d->n_kv_heads * a2ats::append_parts(n_new, blocks->block) * 2 >= (1LL << 31)) return A2ATS_ERR_UNSUPPORTED;
+  if (!launchable(*d, d->n_kv_heads, 2 * a2ats::append_parts(n_new, blocks->block), 512)) return A2ATS_ERR_UNSUPPORTED;
   const hipError_t e = a2ats::launch_append(*d, m, blocks->kv_dtype, blocks->format, rows, k_new, v_new, n_new, seq_lens,
                                             new_lens, (hipStream_t)stream);
   return e == hipSuccess ? A2ATS_OK : A2ATS_ERR_HIP;
@@ -718,10 +723,11 @@ int a2ats_block_topk(const a2ats_dims* d, const a2ats_kv_blocks* blocks, const v
   if (top_blocks < 0 || window < 0 || n_sink < 0) return A2ATS_ERR_INVALID_ARG;
   if (top_blocks > 4096) return A2ATS_ERR_UNSUPPORTED;
   if (!q || !cos_b || !sin_b || !q_rot || !block_count || (top_blocks > 0 && !block_idx)) return A2ATS_ERR_INVALID_ARG;
-  if ((token_idx == nullptr) != (token_count == nullptr)) return A2ATS_ERR_INVALID_ARG;
+  if (top_blocks > 0 && (token_idx == nullptr) != (token_count == nullptr)) return A2ATS_ERR_INVALID_ARG;
   if (misaligned16(q) || misaligned16(cos_b) || misaligned16(sin_b) || misaligned16(q_rot)) return A2ATS_ERR_INVALID_ARG;
   const a2ats::BlockTopkPlan plan = a2ats::make_block_topk_plan(*d, blocks->block, shared != 0);
-  if ((int64_t)d->batch * d->n_kv_heads * plan.chunks >= (1LL << 31)) return A2ATS_ERR_UNSUPPORTED;
+  if (!launchable(*d, d->n_kv_heads, plan.chunks, 256) || !launchable(*d, shared ? d->n_kv_heads : d->n_q_heads, 1, 1024))
+    return A2ATS_ERR_UNSUPPORTED;
   if (plan.bytes > 0 && (!ws || misaligned16(ws) || ws_bytes < plan.bytes)) return A2ATS_ERR_WORKSPACE;
   const hipError_t e = a2ats::launch_block_topk(*d, m, blocks->kv_dtype, q, cos_b, sin_b, q_rot, shared != 0, top_blocks, window,
                                                 n_sink, seq_lens, block_idx, block_count, block_score, token_idx, token_count,
@@ -745,7 +751,7 @@ int a2ats_sparse_attn_kv8(const a2ats_dims* d, const a2ats_kv_blocks* blocks, co
   if (window > 0 && (!cos_win || !sin_win)) return A2ATS_ERR_INVALID_ARG;
   if (misaligned16(q) || misaligned16(q_rot) || misaligned16(cos_win) || misaligned16(sin_win)) return A2ATS_ERR_INVALID_ARG;
   const a2ats::Kv8Plan plan = a2ats::make_kv8_plan(*d, (long)n_sel * sel_size, window, shared != 0);
-  if ((int64_t)d->batch * d->n_q_heads * plan.parts >= (1LL << 31)) return A2ATS_ERR_UNSUPPORTED;
+  if (!launchable(*d, d->n_q_heads, plan.parts, 256)) return A2ATS_ERR_UNSUPPORTED;
   if (plan.bytes > 0 && (!ws || misaligned16(ws) || ws_bytes < plan.bytes)) return A2ATS_ERR_WORKSPACE;
   const hipError_t e = a2ats::launch_sparse_attn_kv8(*d, m, blocks->kv_dtype, blocks->format, q, q_rot, sel_idx, sel_count, n_sel,
                                                      log2_of(sel_size), shared != 0, window, n_sink, cos_win, sin_win, seq_lens,

@@ -663,7 +663,7 @@ __global__ __launch_bounds__(kPickThreads) void pick_blocks_kernel(TopkArgs a) {
       }
     }
   }
-  if (a.token_idx == nullptr) return;   // (uniform)
+  if (a.token_count == nullptr) return;   // (uniform)
   // The tokens: whole blocks but for the first and the last candidate block, of which the candidates are taken.
   const int blk = 1 << shift, slots = a.top_blocks << shift;
   const int skip = kk > 0 && s_sel[0] == first ? sr.sink_end - (first << shift) : 0;

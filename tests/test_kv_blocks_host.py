@@ -108,6 +108,20 @@ def test_arguments_that_are_refused(B):
     assert need > 0 and attn(B, d=long, n_sel=2048, window=64) == -3 and attn(B, d=long, n_sel=2048, window=64, ws=ONE, ws_bytes=64) == -3
 
 
+def test_calls_of_nothing(B):
+    """No new tokens, or no blocks to select: the empty arrays may have no address."""
+    one = dims(B, batch=1)
+    assert append(B, d=one, k=None, v=None, n_new=0) == 0 and bounds(B, d=one, k=None, n_new=0) == 0
+    assert topk(B, top=0, idx=None, tok=None, ntok=ONE) == 0
+
+
+def test_grids_that_are_too_large_are_refused(B):
+    """Launches of 2^32 threads or more."""
+    many = dims(B, batch=1 << 20, heads=8, kv_heads=8)
+    assert append(B, d=many) == -2 and topk(B, d=many) == -2
+    assert attn(B, d=dims(B, batch=1 << 21, heads=8, kv_heads=8)) == -2
+
+
 def test_workspaces_cover_their_calls(B):
     """The figure for the smallest blocks and 64 sinks is enough for every block size, kind of selection and fewer sinks: found by
     asking the calls, which refuse what is too small (a batch of one, so that nothing is launched: ws misaligned at the figure)."""
