@@ -369,7 +369,8 @@ class KvBlocks:
     k_scale, ...   float32 [.., ctx_stride / block] (pages: page_size / block)
     k_tail, ...    kv_dtype [B, Hkv, block, D]
     bounds         kv_dtype [.., ctx_stride / block, 2, D] (pages: page_size / block)
-    All of k .. v_tail are None for a cache of which only the bounds are kept here (key_bounds, block_topk)."""
+    All of k .. v_tail are None for a cache of which only the bounds are kept here (key_bounds, block_topk).
+    The tensors and their memory stay those that were given: a cache in other memory is another KvBlocks."""
 
     def __init__(self, dims: Dims, block: int, kv_dtype: torch.dtype, k=None, v=None, k_scale=None, v_scale=None, k_tail=None,
                  v_tail=None, bounds=None, page_table=None, page_size: int = 0):

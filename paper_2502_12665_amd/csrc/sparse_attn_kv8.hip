@@ -130,8 +130,8 @@ __device__ __forceinline__ int row_exponent(const float (&x)[32], bool& ok) {
   return max((int)(big >> 23) - 126, -100);
 }
 
-// A query as float16 terms, for the columns of the first three (eight heads: two): x = 2^(e - 8) (t0 + t1 + t2), all bits of it
-// that are above 2^-24 (2^-14 of the least term) of 2^e.  Returns 2^(e - 8).
+// A query as float16 terms, for the columns of the first three (eight heads: two): x = 2^(e - 8) (t0 + t1 + t2) but for 2^-33 of 2^e
+// (half the least float16; eight heads: 2^-22).  Returns 2^(e - 8).
 template <int GP>
 __device__ __forceinline__ float query_terms(const float (&x)[32], int term, bool active, f16x8 (&q)[4]) {
   bool ok;
@@ -171,10 +171,11 @@ struct PairRows {
   uint4 k[2][2];
   uint2 v[8];
 };
-// Where the rows of two pairs are in the cache, their scales, and 0 or, for a place without a row, -inf: of a wave, in LDS.
+// Where the rows of two pairs are in the cache, their scales, and 0 or, for a place without a row, all bits: of a wave, in LDS.
 struct PairPlaces {
   uint32_t row[2 * kPair];
-  float ks[2 * kPair], vs[2 * kPair], none[2 * kPair];
+  float ks[2 * kPair], vs[2 * kPair];
+  uint32_t none[2 * kPair];
 };
 
 // Eight rows of the incomplete block, one for each group of 8 lanes, and a head's query for them: elements 8 * (lane of the group)
@@ -220,11 +221,13 @@ __device__ __forceinline__ void pair_weights(const f32x4 (&dot)[2], const PairPl
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     const int at = first + t * 16 + lrow * 4;
-    const float4 k4 = *(const float4*)(pl.ks + at), v4 = *(const float4*)(pl.vs + at), n4 = *(const float4*)(pl.none + at);
-    const float kk[4] = {k4.x, k4.y, k4.z, k4.w}, vv[4] = {v4.x, v4.y, v4.z, v4.w}, nn[4] = {n4.x, n4.y, n4.z, n4.w};
+    const float4 k4 = *(const float4*)(pl.ks + at), v4 = *(const float4*)(pl.vs + at);
+    const uint4 n4 = *(const uint4*)(pl.none + at);
+    const float kk[4] = {k4.x, k4.y, k4.z, k4.w}, vv[4] = {v4.x, v4.y, v4.z, v4.w};
+    const uint32_t nn[4] = {n4.x, n4.y, n4.z, n4.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      lg[4 * t + i] = __builtin_fmaf(dot[t][i], kk[i], nn[i]);
+      lg[4 * t + i] = __uint_as_float((nn[i] & 0xff800000u) | (~nn[i] & __float_as_uint(dot[t][i] * kk[i])));   // (-inf)
       vsc[4 * t + i] = vv[i];
     }
   }
@@ -525,7 +528,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   auto put_scales = [&](PairPlaces& to, const Place& pc) {
     to.ks[lane] = pc.in ? pc.ks : 0.f;
     to.vs[lane] = pc.in ? pc.vs : 0.f;
-    to.none[lane] = pc.in ? 0.f : -INFINITY;
+    to.none[lane] = pc.in ? 0u : ~0u;
   };
   PairPlaces &wp = s.places.win[wv], *fp = s.places.far[wv];
   auto place_far = [&](PairPlaces& to, int pair) {   // this pair and the next one

@@ -305,6 +305,14 @@ def test_select_of_many_blocks(ctx, blk, top):
         check_select(c, o, shared, top, 100, 3, bounds=[[bd.double()]])
 
 
+def test_select_of_no_blocks_says_so():
+    """K 0: empty lists, whose arrays have no address, and counts of zero."""
+    c = Case([100, 0], 4, 2, 16, "i8", "bf16", seed=34)
+    c.append(c.lens)
+    o = run_select(c, False, 0, 3, 1, tokens=True)
+    assert (o["count"] == 0).all() and (o["n_tokens"] == 0).all()
+
+
 def test_select_survives_what_is_not_finite():
     """K' blocks are selected whatever the scores are worth, and a score that is no number counts as infinite."""
     c = Case([40 * 16], 2, 1, 16, "i8", "f32", seed=35)
@@ -506,6 +514,24 @@ def test_what_is_not_finite_shows():
     assert got[0, 0].isnan().all() and torch.isfinite(got[0, 1]).all() and torch.isfinite(got[1]).all()
     sel = [[[2], [1]], [[1], [1]]]
     assert torch.isfinite(run_attend(c, sel, 16, False, 16, 0)[0]).all()
+
+
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_that_are_not_attended_do_not_count(fmt, dtype):
+    """A query that is no number: NaN where something is attended, zeros where nothing is, other heads as they were."""
+    c = Case([200, 200], 4, 2, 16, fmt, dtype, seed=77, bounds=False)
+    c.append(c.lens)
+    none = [-1, 13, 1 << 20]
+    sel = [[[2], none, [3], [4]], [[2], [], none, [5]]]
+    fine = run_attend(c, sel, 16, False, 0, 0)[0]
+    q_rot = run_attend(c, sel, 16, False, 0, 0)[1]
+    for bad in (math.nan, math.inf):
+        wrong = q_rot.clone()
+        wrong[:, 1:3, 5] = bad
+        got = run_attend(c, sel, 16, False, 0, 0, q_rot=wrong)[0]
+        assert (got[0, 1] == 0).all() and (got[1, 1] == 0).all() and (got[1, 2] == 0).all() and got[0, 2].isnan().all()
+        assert torch.equal(got[:, [0, 3]], fine[:, [0, 3]])
 
 
 def test_large_logits():
