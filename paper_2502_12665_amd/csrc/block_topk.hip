@@ -28,7 +28,6 @@ namespace a2ats {
 namespace {
 
 constexpr int kScoreThreads = 256;
-constexpr int kPickThreads = 1024;
 constexpr int kPickBins = 2048;
 constexpr int kBandMost = 1024;
 constexpr int kD = kRowBytes;
@@ -382,9 +381,9 @@ __global__ __launch_bounds__(kScoreThreads) void score_blocks_kernel(TopkArgs a)
 
 // MATRIX: the scores are those of the matrix cores.  PER: scores of a thread, in registers; 0: they are read again in every
 // pass.
-template <typename T, bool MATRIX, int PER>
-__global__ __launch_bounds__(kPickThreads) void pick_blocks_kernel(TopkArgs a) {
-  constexpr int NT = kPickThreads, NW = NT / 64, KEEP = PER > 0 ? PER : 1;
+template <typename T, bool MATRIX, int NT, int PER>
+__global__ __launch_bounds__(NT) void pick_blocks_kernel(TopkArgs a) {
+  constexpr int NW = NT / 64, KEEP = PER > 0 ? PER : 1;
   __shared__ uint32_t s_hist[kPickBins], s_a[NW], s_b[NW], s_res[2], s_lo, s_hi, s_band, s_big;
   __shared__ uint32_t s_band_key[kBandMost];
   __shared__ uint16_t s_band_at[kBandMost];
@@ -630,7 +629,7 @@ __global__ __launch_bounds__(kPickThreads) void pick_blocks_kernel(TopkArgs a) {
   }
   __syncthreads();
   // The selection in ascending order: how many there are before each wave's blocks of a round.
-  uint32_t* s_before = s_hist;   // [round][wave], at most 64 * 16
+  uint32_t* s_before = s_hist;   // [round][wave], at most 1024
   if (wv == 0) {
     uint32_t run = 0;
     for (int i = round_first * NW; i < round_end * NW; i += 64) {
@@ -700,14 +699,30 @@ static void launch_f64(const TopkArgs& a, hipStream_t stream) {
   else hipLaunchKernelGGL((score_blocks_f64_kernel<G, false>), grid, block, 0, stream, a);
 }
 
+template <typename T, bool MATRIX, int NT, int PER>
+static hipError_t launch_pick_as(const TopkArgs& a, int batch, hipStream_t stream) {
+  const size_t lds = ((size_t)(a.total_blocks + NT - 1) / NT * (NT / 32) + a.top_blocks) * sizeof(uint32_t);
+  hipLaunchKernelGGL((pick_blocks_kernel<T, MATRIX, NT, PER>), dim3((unsigned)(batch * a.heads)), dim3(NT), lds, stream, a);
+  return hipGetLastError();
+}
+// Threads of a head's workgroup: it is a chain of short phases, each of which a small workgroup ends sooner and leaves room for
+// others on its CU.  Both launches of a call (bfloat16, 4 heads a KV head, an eighth of the blocks selected, at most 128), us, with the
+// threads taken and with 1024:
+//   blocks   256: 128 heads  9.8 (11.1), 896 heads 20.0 (36.6)       2048: 128 heads 17.5 (17.9), 896 heads  68.3 (79.7)
+//   blocks  1024: 128 heads 13.4 (13.8), 512 heads 22.1 (27.6),      4096: 128 heads 23.3 (23.0), 896 heads 121.4 (132.9)
+//                 896 heads 33.8 with 256 threads, 38.8 with 512, 49.6
+//   blocks  8192: 128 heads 35.1 with 1024, 37.3 with 512; 512 heads 131.5 and 126.3
 template <typename T, bool MATRIX>
 static hipError_t launch_pick(const TopkArgs& a, int batch, hipStream_t stream) {
-  const size_t lds = ((size_t)(a.total_blocks + kPickThreads - 1) / kPickThreads * (kPickThreads / 32) + a.top_blocks) * sizeof(uint32_t);
-  const dim3 grid((unsigned)(batch * a.heads)), block(kPickThreads);
-  if (a.total_blocks <= 2 * kPickThreads) hipLaunchKernelGGL((pick_blocks_kernel<T, MATRIX, 2>), grid, block, lds, stream, a);
-  else if (a.total_blocks <= 8 * kPickThreads) hipLaunchKernelGGL((pick_blocks_kernel<T, MATRIX, 8>), grid, block, lds, stream, a);
-  else hipLaunchKernelGGL((pick_blocks_kernel<T, MATRIX, 0>), grid, block, lds, stream, a);
-  return hipGetLastError();
+  const long heads = (long)batch * a.heads;
+  if (a.total_blocks <= 256) return launch_pick_as<T, MATRIX, 256, 1>(a, batch, stream);
+  if (a.total_blocks <= 1024)
+    return heads > 512 ? launch_pick_as<T, MATRIX, 256, 4>(a, batch, stream) : launch_pick_as<T, MATRIX, 512, 2>(a, batch, stream);
+  if (a.total_blocks <= 2048) return launch_pick_as<T, MATRIX, 512, 4>(a, batch, stream);
+  if (a.total_blocks <= 4096) return launch_pick_as<T, MATRIX, 512, 8>(a, batch, stream);
+  if (a.total_blocks <= 8192)
+    return heads > 256 ? launch_pick_as<T, MATRIX, 512, 16>(a, batch, stream) : launch_pick_as<T, MATRIX, 1024, 8>(a, batch, stream);
+  return launch_pick_as<T, MATRIX, 1024, 0>(a, batch, stream);
 }
 
 hipError_t launch_block_topk(const a2ats_dims& d, const BlockCache& m, int kv_dtype, const void* q, const float* cos_b,

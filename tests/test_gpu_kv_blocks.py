@@ -305,6 +305,26 @@ def test_select_of_many_blocks(ctx, blk, top):
         check_select(c, o, shared, top, 100, 3, bounds=[[bd.double()]])
 
 
+@pytest.mark.parametrize("batch, blocks, dtype", [(9, 200, "bf16"), (9, 700, "bf16"), (5, 5000, "bf16"), (5, 5000, "f32"), (9, 1500, "f32")])
+def test_select_of_many_heads(batch, blocks, dtype):
+    """More heads than CUs, of which smaller workgroups are made; bounds drawn directly, sequences of different lengths."""
+    blk, Hq, Hkv = 16, 64, 8
+    ctx = blocks * blk
+    c = Case.__new__(Case)
+    c.batch, c.heads, c.kv_heads, c.G, c.blk, c.page, c.dims = batch, Hq, Hkv, 8, blk, 0, dims_of(batch, Hq, Hkv, ctx, ctx)
+    c.have = [ctx] + [ctx - 37 * b * b for b in range(1, batch)]
+    c.inv = synth.inv_freq(D, 500000.0)
+    g = gen(blocks)
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    c.q = torch.randn(batch, Hq, D, generator=g).to(dt)
+    mid = torch.randn(batch, Hkv, blocks, D, generator=g) * 0.5
+    bd = torch.stack([mid - 2, mid + 2], 3).to(dt)
+    c.cache = B.KvBlocks(c.dims, blk, dt, bounds=bd.cuda())
+    o = run_select(c, False, 50, 30, 20)
+    bounds = [[bd[b, kv, : -(-c.have[b] // blk)].double() for kv in range(Hkv)] for b in range(batch)]
+    check_select(c, o, False, 50, 30, 20, bounds=bounds)
+
+
 def test_select_of_no_blocks_says_so():
     """K 0: empty lists, whose arrays have no address, and counts of zero."""
     c = Case([100, 0], 4, 2, 16, "i8", "bf16", seed=34)
