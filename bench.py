@@ -540,6 +540,64 @@ def group_shared_step(args, torch, B, synth, wl):
     }))
 
 
+def block_cache_step(args, torch, B, synth, wl):
+    """A decode step over a cache in 8 bits cut into blocks of 16 tokens (no codebook): a2ats_kv8_append of the current token,
+    a2ats_block_topk of as many blocks as hold the workload's top_k tokens, a2ats_sparse_attn_kv8 over them and the window;
+    with --group-shared one selection per KV head."""
+    blk, N, K, w = 16, wl.ctx_len, wl.top_k, wl.window
+    dims = B.make_dims(wl.batch, wl.n_q_heads, wl.n_kv_heads, wl.head_dim, wl.n_sub, N, (N + blk - 1) // blk * blk)
+    codes = torch.int8 if args.block_cache == "i8" else torch.float8_e4m3fn
+    R = max(1, args.replicas)
+    reps = []
+    for r in range(R):
+        x = synth.make_decode_inputs(wl.replace(seed=wl.seed + r), device="cuda")
+        cache = B.KvBlocks.empty(dims, blk, x["q"].dtype, codes)
+        B.kv8_append(dims, cache, x["k"], x["v"], N)
+        st = B.BlockDecodeState(dims, cache, -(-K // blk), w, wl.n_sink, x["inv_freq"], wl.wrope_b, args.group_shared,
+                                scores=False)
+        reps.append((st, x["q"], x["k"][:, :, -1:].contiguous(), x["v"][:, :, -1:].contiguous()))
+        del x
+
+    def step(i):   # (the last token is appended again: its block is in the tail, and is rounded to the same codes)
+        st, q, k_new, v_new = reps[i % R]
+        st.step(q, k_new, v_new)
+
+    def timed(call, n):
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
+        for i in range(n):
+            call(i)
+        torch.cuda.synchronize()
+        return (time.perf_counter() - t0) * 1e3
+
+    for i in range(max(args.warmup, R)):
+        step(i)
+    ms_eager = timed(step, args.steps) / args.steps
+    choices = [(ms_eager, "eager")]
+    if not args.no_graph and args.steps % R == 0:
+        big = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(big):
+            for r in range(R):
+                step(r)
+        big.replay()
+        choices.append((timed(lambda i: big.replay(), args.steps // R) / args.steps, f"replay of one hip graph holding {R} steps"))
+    ms, launch = min(choices)
+    heads = wl.n_kv_heads if args.group_shared else wl.n_q_heads
+    bounds_bytes = wl.batch * wl.n_kv_heads * (N // blk) * 2 * wl.head_dim * reps[0][1].element_size()
+    attn_bytes = wl.batch * heads * (K + w) * 2 * wl.head_dim
+    print(json.dumps({
+        "metric": "cached keys/s = B * Hkv * N / time of a WHOLE decode step over an 8-bit cache (append 1 token + block selection + "
+                  "sparse attention)",
+        "value": wl.batch * wl.n_kv_heads * N / (ms * 1e-3), "unit": "keys/s", "n_gpus": 1, "steps": args.steps,
+        "warmup": args.warmup, "ms_per_step": ms, "launch": launch, "ms_per_step_eager": ms_eager, "higher_is_better": True,
+        "scaling": "weak", "vs_baseline": None, "dtype": f"{args.block_cache} K/V, f32 accumulate; {wl.kv_dtype} bounds, f64 decisions",
+        "data": "synthetic",
+        "config": {"workload": wl.name, "block": blk, "top_blocks": -(-K // blk), "window": w, "group_shared": args.group_shared,
+                   "replicas_cycled": R},
+        "algorithmic_bytes": {"bounds": bounds_bytes, "attended_rows": attn_bytes},
+        "GBps": (bounds_bytes + attn_bytes) / (ms * 1e-3) / 1e9}))
+
+
 def codebook_fit(args, torch, B, synth, wl):
     """Offline codebook construction: one Lloyd iteration under the query-aware distortion (assignment by
     a2ats_encode_keys with the full matrix H, centroid step by a2ats_codebook_update) over whole sequences,
@@ -654,6 +712,9 @@ def main():
     ap.add_argument("--paged-codes", type=int, default=0,
                     help="time the score/top-K phase over a code matrix in pages of this many tokens beside the "
                          "contiguous one; prints a line of its own")
+    ap.add_argument("--block-cache", choices=["i8", "e4m3"],
+                    help="decode steps over a cache in 8 bits cut into blocks, which bounds of the keys select (with "
+                         "--group-shared: one selection per KV head); prints a line of its own")
     ap.add_argument("--encode-prefill", action="store_true",
                     help="measure the prefill-side key encoder (configuration 5 geometry, 8 of its 32 "
                          "sequences) instead of the decode step, and print its own JSON line")
@@ -680,6 +741,9 @@ def main():
         return
     if args.encode_prefill:
         encode_prefill(args, torch, B, synth)
+        return
+    if args.block_cache:
+        block_cache_step(args, torch, B, synth, wl)
         return
     if args.group_shared:
         group_shared_step(args, torch, B, synth, wl)

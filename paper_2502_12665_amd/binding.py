@@ -604,10 +604,11 @@ class DecodeState:
 
 
 class BlockDecodeState:
-    """Device buffers for decode steps over a KvBlocks cache (allocation only; no arithmetic)."""
+    """Device buffers for decode steps over a KvBlocks cache (allocation only; no arithmetic).  scores: whether a step leaves the
+    selected blocks' scores in block_score (which the attention does not need)."""
 
     def __init__(self, dims: Dims, cache: KvBlocks, top_blocks: int, window: int, n_sink: int, inv_freq: torch.Tensor,
-                 wrope_b: int, shared: bool = False):
+                 wrope_b: int, shared: bool = False, scores: bool = True):
         self.dims, self.cache, self.top_blocks, self.window, self.n_sink, self.shared = dims, cache, top_blocks, window, n_sink, shared
         B, Hq, D, dev = dims.batch, dims.n_q_heads, dims.head_dim, cache.device
         heads = dims.n_kv_heads if shared else Hq
@@ -615,7 +616,7 @@ class BlockDecodeState:
         self.q_rot = torch.empty(B, Hq, D, dtype=torch.float32, device=dev)
         self.block_idx = torch.empty(B, heads, top_blocks, dtype=torch.int32, device=dev)
         self.block_count = torch.empty(B, heads, dtype=torch.int32, device=dev)
-        self.block_score = torch.empty(B, heads, top_blocks, dtype=torch.float32, device=dev)
+        self.block_score = torch.empty(B, heads, top_blocks, dtype=torch.float32, device=dev) if scores else None
         self.out = torch.empty(B, Hq, D, dtype=cache.kv_dtype, device=dev)
         n_ws = max(workspace_bytes(dims, OP_BLOCK_TOPK), workspace_bytes(dims, OP_ATTN_KV8, top_blocks * cache.block, window), 256)
         self.ws = torch.empty(n_ws, dtype=torch.uint8, device=dev)
