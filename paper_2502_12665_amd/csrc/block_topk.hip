@@ -401,6 +401,16 @@ __global__ __launch_bounds__(NT) void pick_blocks_kernel(TopkArgs a) {
   float raw[KEEP];
 #pragma unroll
   for (int i = 0; i < PER; ++i) raw[i] = a.scores[(size_t)bh * a.total_blocks + min(tid + i * NT, max(a.total_blocks - 1, 0))];
+  // ... and so are the first query and the chunks' magnitudes (two chunks a thread hold all of them).
+  const int d0 = (lane & 15) * 8, group = tid >> 4;
+  const uint32_t* largest = a.largest + ((size_t)b * a.cache.n_kv_heads + kv) * a.chunks;
+  float q_raw[8];
+  uint32_t large_raw[2] = {0u, 0u};
+  if constexpr (MATRIX) {
+    load8(a.q_rot + q_first * kD + d0, q_raw);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) large_raw[i] = largest[min(tid + i * NT, a.chunks - 1)];
+  }
   const SeqRange sr = seq_range(a.ctx_len, a.seq_lens, b, a.window, a.n_sink, 0);
   int first, last;
   candidate_blocks(sr, shift, first, last);
@@ -430,21 +440,22 @@ __global__ __launch_bounds__(NT) void pick_blocks_kernel(TopkArgs a) {
     __syncthreads();
     const int chunk = chunk_blocks(n, a.chunks);
     uint32_t big = 0u;   // (as bits: what is not a number is the largest)
-    for (int i = tid; i < a.chunks; i += NT)
-      if (i * chunk < n) big = max(big, a.largest[((size_t)b * a.cache.n_kv_heads + kv) * a.chunks + i]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (tid + i * NT < a.chunks && (tid + i * NT) * chunk < n) big = max(big, large_raw[i]);
     big = wave_max_to_last_lane(big);
     if (lane == 63 && wv < (a.chunks + 63) / 64) atomicMax(&s_big, big);
   }
   __syncthreads();
 
   // This group of 16 lanes' part of the head's query, for float64 scores.
-  const int d0 = (lane & 15) * 8, group = tid >> 4;
   ExactQuery<1, true> eq;
   if constexpr (MATRIX) {
-    for (int g = 0; g < n_sum; ++g) {
+    eq.add(0, true, q_raw);
+    for (int g = 1; g < n_sum; ++g) {
       float r[8];
       load8(a.q_rot + (q_first + g) * kD + d0, r);
-      eq.add(0, g == 0, r);
+      eq.add(0, false, r);
     }
   }
   auto exact_score = [&](int c) {   // of block c, by 16 lanes
