@@ -19,6 +19,11 @@
 // are not.  The others, a handful, get their float64 scores, and are ranked by these (equal scores: the lower block first).
 // float32 bounds are scored in float64 right away (e = 0).  A band of more than kBandMost blocks (many equal scores, or bounds
 // that are not finite) has all blocks of the head scored in float64 and a select over all digits.
+//
+// Two launches: the scores, and a workgroup a head that selects from them.  Measured, 4 x 8 KV heads of 8192 blocks, 4 heads
+// each: scores 27.7 us = 4.85 TB/s of 134 MB (the rate of a large copy), selection 11 (a chain of a dozen phases of 0.5 to 2 us:
+// range, one digit, band, its exact scores, ranks, output).  Selecting in the last of a head's score workgroups, one launch
+// for both, was slower: its phases do not overlap the stream of the others by as much as they then cost.
 #include <algorithm>
 
 #include "internal.hpp"

@@ -8,7 +8,15 @@
 //
 // The call is a stream, 2 * 128 * e bytes read and 2 * 128 written per token and KV head, so a row is read once:
 // a wave keeps 16 rows in registers (32 floats a lane), a workgroup of 4 waves 64 rows (of 8 for blocks of 128);
-// the largest magnitude of a block goes from wave to wave through LDS, and the rows are rounded where they are.
+// the largest magnitude of a block goes from wave to wave through LDS, and the rows are rounded where they are.  What is
+// not 127 x / a at once (a code within the product's error of a half) is decided exactly, in float64 or, for bfloat16, whose
+// products cannot come that close without being a half, by cutting the product to 20 bits.
+//
+// Measured: 8 KV heads x 32768 tokens, bfloat16 to int8 with bounds, 49 us = 4.2 TB/s of 206 MB, of which the bounds' minima and
+// maxima (vector ALU) are 8; e4m3 without bounds runs at the rate of a large copy (4.9 TB/s).  4 x 4 x 4099 tokens, float32 to
+// e4m3 in pages, 13.6 - 15 us = 3.4 - 3.8 TB/s.  One token of 16 x 8 heads: 4.7 us, of which an empty launch is 1.6; the rest are the
+// requests that wait for each other (length, rows, bounds).  Requesting the bounds and the tail's rows ahead of the barrier did
+// not shorten it (4.9).
 #include "internal.hpp"
 #include "kv_blocks.hpp"
 

@@ -19,6 +19,12 @@
 // Window rows are turned back by their distance, (q R_delta) . k = q . (k R_-delta), and go in as two float16 terms.  What is
 // left in the tail, at most a block, is done on the vector ALU.
 // The statistics, all sums and the output are float32.  Logits are kept times log2 e, so that a weight is one exponential.
+//
+// Measured: 32 x 28 heads of 2176 rows, e4m3, 97 - 101 us = 4.9 - 5.1 TB/s of 497 MB (the rate of a large copy); the same rows of int8
+// 91 us; 4 x 32 heads of 2304 rows, int8, in 4 parts 21 us = 3.4 TB/s with the merge of 2.5; one selection for 4 heads, 16 x 8 of
+// 1152 rows in pages, in 2 parts 20.5 us = 1.9 TB/s: few rows, and requests that wait for each other (length and index, page, row),
+// of which a wave has two pairs of rows in flight.  More in flight does not fit: 128 registers for four waves a SIMD spill, and
+// a spill waits for all loads (three times slower), so there are two waves a SIMD with 256.
 #include <algorithm>
 #include <cfloat>
 
