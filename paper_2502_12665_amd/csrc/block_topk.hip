@@ -392,6 +392,7 @@ __global__ __launch_bounds__(NT) void pick_blocks_kernel(TopkArgs a) {
   __shared__ uint32_t s_hist[kPickBins], s_a[NW], s_b[NW], s_res[2], s_lo, s_hi, s_band, s_big;
   __shared__ uint32_t s_band_key[kBandMost];
   __shared__ uint16_t s_band_at[kBandMost];
+  __shared__ double2 s_query[MATRIX ? kD : 1];   // of several heads: the sums of their queries and of the magnitudes
   extern __shared__ uint32_t s_dyn[];   // a bit for each block that is taken out of the band; then the selection
   // (on the XCD where the head's scores have been written)
   const int of = a.shared ? 1 : a.group;
@@ -406,13 +407,19 @@ __global__ __launch_bounds__(NT) void pick_blocks_kernel(TopkArgs a) {
   float raw[KEEP];
 #pragma unroll
   for (int i = 0; i < PER; ++i) raw[i] = a.scores[(size_t)bh * a.total_blocks + min(tid + i * NT, max(a.total_blocks - 1, 0))];
-  // ... and so are the first query and the chunks' magnitudes (two chunks a thread hold all of them).
+  // ... and so are the queries (of one head: this lane's eight dimensions; of several: a dimension of each for a thread) and the
+  // chunks' magnitudes (two chunks a thread hold all of them).
   const int d0 = (lane & 15) * 8, group = tid >> 4;
   const uint32_t* largest = a.largest + ((size_t)b * a.cache.n_kv_heads + kv) * a.chunks;
   float q_raw[8];
   uint32_t large_raw[2] = {0u, 0u};
   if constexpr (MATRIX) {
-    load8(a.q_rot + q_first * kD + d0, q_raw);
+    if (n_sum == 1) {
+      load8(a.q_rot + q_first * kD + d0, q_raw);
+    } else if (tid < kD) {
+#pragma unroll
+      for (int g = 0; g < 8; ++g) q_raw[g] = a.q_rot[(q_first + min(g, n_sum - 1)) * kD + tid];
+    }
 #pragma unroll
     for (int i = 0; i < 2; ++i) large_raw[i] = largest[min(tid + i * NT, a.chunks - 1)];
   }
@@ -450,17 +457,29 @@ __global__ __launch_bounds__(NT) void pick_blocks_kernel(TopkArgs a) {
       if (tid + i * NT < a.chunks && (tid + i * NT) * chunk < n) big = max(big, large_raw[i]);
     big = wave_max_to_last_lane(big);
     if (lane == 63 && wv < (a.chunks + 63) / 64) atomicMax(&s_big, big);
+    if (n_sum > 1 && tid < kD) {
+      double q = 0.0, mag = 0.0;
+#pragma unroll
+      for (int g = 0; g < 8; ++g) {
+        q += g < n_sum ? (double)q_raw[g] : 0.0;
+        mag += g < n_sum ? (double)fabsf(q_raw[g]) : 0.0;
+      }
+      s_query[tid] = make_double2(q, mag);
+    }
   }
   __syncthreads();
 
   // This group of 16 lanes' part of the head's query, for float64 scores.
   ExactQuery<1, true> eq;
   if constexpr (MATRIX) {
-    eq.add(0, true, q_raw);
-    for (int g = 1; g < n_sum; ++g) {
-      float r[8];
-      load8(a.q_rot + (q_first + g) * kD + d0, r);
-      eq.add(0, false, r);
+    if (n_sum == 1) {
+      eq.add(0, true, q_raw);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        eq.q[0][e] = s_query[d0 + e].x;
+        eq.mag[0][e] = s_query[d0 + e].y;
+      }
     }
   }
   auto exact_score = [&](int c) {   // of block c, by 16 lanes
