@@ -711,6 +711,30 @@ def test_block_selection_for_a_cache_that_is_not_in_8_bits(shared):
             assert (err <= off + more + 2.0 ** -8 * (want.abs() + off)).all(), (b, h, float(err.max()))
 
 
+def test_lengths_outside_of_their_range_are_limited():
+    """seq_lens below 0 and above ctx_len, new_lens below 0, above n_new and above the sequence's length: taken as the nearest that can be."""
+    c = Case([96, 96, 96, 96], 4, 2, 32, "i8", "bf16", seed=95)
+    want = Case([96, 96, 0, 10], 4, 2, 32, "i8", "bf16", seed=95)
+    new = [torch.stack(t).cuda() for t in (c.k, c.v)]
+    lens = torch.tensor([1000, 96, -7, 10], dtype=torch.int32, device="cuda")
+    news = torch.tensor([2000, -3, 50, 96], dtype=torch.int32, device="cuda")
+    for cache, sl, nl in ((c.cache, lens, news), (want.cache, [96, 96, 0, 10], [96, 0, 0, 10])):
+        a, b = (x if torch.is_tensor(x) else torch.tensor(x, dtype=torch.int32, device="cuda") for x in (sl, nl))
+        B.kv8_append(c.dims, cache, *new, 96, a, b)
+    torch.cuda.synchronize()
+    for x in ("k", "v", "k_scale", "v_scale", "k_tail", "v_tail", "bounds"):
+        assert torch.equal(getattr(c.cache, x), getattr(want.cache, x)), x
+    c.append([96, 96, 96, 96])                             # (the rest, so that every row may be attended)
+    sel = [[[0, 2]] * 4] * 4
+    outs = []
+    for have in ([1000, 96, -7, 96], [96, 96, 0, 96]):
+        c.have = have
+        outs.append(run_attend(c, sel, 32, False, 7, 1)[0])
+    assert torch.equal(*outs) and (outs[0][2] == 0).all()
+    o, p = run_select(c, False, 2, 7, 1, lens=[1000, 96, -7, 96]), run_select(c, False, 2, 7, 1, lens=[96, 96, 0, 96])
+    assert all(torch.equal(o[x], p[x]) for x in o) and (o["count"][2] == 0).all()
+
+
 def test_a_pool_of_more_than_4_gib():
     """Pages behind the first 2^32 bytes of a pool: append, select and attend there."""
     page, blk, Hkv = 64, 32, 8
