@@ -1,0 +1,75 @@
+"""Attention over a cache in 8 bits: the terms that its operands are split into are all there, for every number of heads that
+attend the same rows (tests/kv_terms.py)."""
+import pytest
+import torch
+
+from paper_2502_12665_amd import binding as B
+from tests import kv_terms as K
+
+pytestmark = pytest.mark.gpu
+D = 128
+CODES = {"i8": torch.int8, "e4m3": torch.float8_e4m3fn}
+
+
+def attend(dims, cache, q, q_rot, sel, size, shared, window, cos_win, sin_win):
+    """sel [B][H] lists of the same number, or of none."""
+    n_sel = max(1, len(sel[0][0]))
+    idx = torch.tensor([[row if row else [-1] for row in rows] for rows in sel], dtype=torch.int32).cuda()
+    cnt = torch.full(idx.shape[:2], len(sel[0][0]), dtype=torch.int32).cuda()
+    ws = torch.empty(max(16, B.workspace_bytes(dims, B.OP_ATTN_KV8, n_sel * size, window)), dtype=torch.uint8, device="cuda")
+    out = torch.full_like(q, 3.0, device="cuda")
+    B.sparse_attn_kv8(dims, cache, q.cuda(), q_rot.cuda(), idx, cnt, n_sel, size, shared, window, 0, cos_win.contiguous().cuda(),
+                      sin_win.contiguous().cuda(), None, out, ws)
+    torch.cuda.synchronize()
+    return out.cpu()
+
+
+def filled(dims, dtype, fmt, k, v, k_scale, v_scale, blk):
+    cache = B.KvBlocks.empty(dims, blk, dtype, CODES[fmt], False)
+    for x, codes, scale in (("k", k, k_scale), ("v", v, v_scale)):
+        getattr(cache, x).copy_(codes.to(CODES[fmt]))
+        getattr(cache, x + "_scale").copy_(scale)
+    return cache
+
+
+@pytest.mark.parametrize("what, fmt, G, shared", K.ALL)
+def test_low_terms_of_queries_and_keys(what, fmt, G, shared):
+    t = K.Terms(what, fmt, G, shared, seed=G)
+    dims = B.make_dims(K.B, t.heads, K.HKV, D, 16, K.N, K.N)
+    cache = filled(dims, torch.float32, fmt, t.k, t.v, t.k_scale, t.v_scale, K.BLK)
+    cos, sin = K.tables(t.window)
+    got = attend(dims, cache, t.q, t.q_rot, t.sel, 1, shared, t.window, cos, sin)
+    for b in range(K.B):
+        for h in range(t.heads):
+            want, tol = t.want(b, h, cos.double(), sin.double())
+            err = (got[b, h].double() - want).abs()
+            assert (err <= tol).all(), (b, h, float((err / tol).max()), float(err.max()))
+
+
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+@pytest.mark.parametrize("G, shared", [(1, False), (4, False), (3, True), (4, True), (5, True), (6, True), (7, True), (8, True)])
+@pytest.mark.parametrize("window", [0, 1])
+def test_weights_have_24_bits(fmt, G, shared, window):
+    """A query of zeros and one row: the weight is that row's v_scale, any float32.  Its three terms hold all of it, their products with a
+    code are exact, and at most three additions follow (a truncated one is off by 2 u), and a division by 1: 7 u < 8 u.  Weights of
+    16 bits are off by up to 2^-16 = 256 u."""
+    batch, n, blk, Hkv = 24, 16, 16, 2
+    heads = Hkv * G
+    g = torch.Generator().manual_seed(G + window)
+    v = torch.randint(-127, 128, (batch, Hkv, n, D), generator=g).float() if fmt == "i8" else \
+        (100 * torch.randn(batch, Hkv, n, D, generator=g)).clamp(-448, 448).to(torch.float8_e4m3fn).float()
+    v_scale = torch.rand(batch, Hkv, 1, generator=g) + 0.01
+    dims = B.make_dims(batch, heads, Hkv, D, 16, n, n)
+    cache = filled(dims, torch.float32, fmt, v, v, v_scale, v_scale, blk)
+    zero = torch.zeros(batch, heads, D)
+    H = Hkv if shared else heads
+    pick = torch.randint(0, n - 1, (batch, H, 1), generator=g)
+    sel = [[[] for _ in range(H)] for _ in range(batch)] if window else pick.tolist()
+    cos, sin = K.tables(window)
+    got = attend(dims, cache, zero, zero, sel, 1, shared, window, cos, sin)
+    for b in range(batch):
+        for h in range(heads):
+            row = n - 1 if window else sel[b][h // G if shared else h][0]
+            want = v[b, h // G, row].double() * v_scale[b, h // G, 0].double()
+            err = (got[b, h].double() - want).abs()
+            assert (err <= 8 * 2.0 ** -24 * want.abs()).all(), (b, h, float((err / want.abs().clamp(min=1e-30)).max() * 2 ** 24))
