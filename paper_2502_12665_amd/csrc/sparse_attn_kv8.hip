@@ -122,8 +122,9 @@ __device__ __forceinline__ void to_logits(float (&x)[32]) {
   for (int i = 0; i < 32; ++i) x[i] *= kLogit;
 }
 
-// The least e >= -100 with |x| < 2^e for all x of a head's row (32 elements in this lane, the others in the lane rows);
-// ok: all are finite.
+// The least e >= -97 with |x| < 2^e for all x of a head's row (32 elements in this lane, the others in the lane rows);
+// ok: all are finite.  (-97: 2^(30 - e), by which an element becomes a whole number, is a float32 then, also for a row of zeros;
+// what is below 2^-30 of 2^-97 is below the least normal number.)
 __device__ __forceinline__ int row_exponent(const float (&x)[32], bool& ok) {
   uint32_t big = 0;
 #pragma unroll
@@ -133,7 +134,7 @@ __device__ __forceinline__ int row_exponent(const float (&x)[32], bool& ok) {
   const auto b = __builtin_amdgcn_permlane16_swap(big, big, false, false);
   big = max(b[0], b[1]);
   ok = big < 0x7f800000u;
-  return max((int)(big >> 23) - 126, -100);
+  return max((int)(big >> 23) - 126, -97);
 }
 
 // A query as float16 terms, for the columns of the first three (eight heads: two): x = 2^(e - 8) (t0 + t1 + t2) but for 2^-33 of 2^e

@@ -73,3 +73,39 @@ def test_weights_have_24_bits(fmt, G, shared, window):
             want = v[b, h // G, row].double() * v_scale[b, h // G, 0].double()
             err = (got[b, h].double() - want).abs()
             assert (err <= 8 * 2.0 ** -24 * want.abs()).all(), (b, h, float((err / want.abs().clamp(min=1e-30)).max() * 2 ** 24))
+
+
+@pytest.mark.parametrize("G, shared", [(4, False), (4, True), (7, True)])
+@pytest.mark.parametrize("fmt, dtype", [("i8", torch.float32), ("i8", torch.bfloat16), ("e4m3", torch.float32)])
+def test_queries_of_zeros_and_tiny_ones(fmt, dtype, G, shared):
+    """Queries of 2^-99 (and of zeros: all rows alike) over keys whose scales make ordinary logits of them."""
+    batch, n, blk, Hkv, rows = 3, 32, 16, 1, 8
+    g = torch.Generator().manual_seed(5)
+    dims = B.make_dims(batch, G, Hkv, D, 16, n, n)
+    k = torch.zeros(batch, Hkv, n, D)
+    k[..., 3] = torch.randint(-100, 101, (batch, Hkv, n), generator=g).float()
+    k[..., 80] = torch.randint(-100, 101, (batch, Hkv, n), generator=g).float()
+    if fmt == "e4m3":
+        k = k.to(torch.float8_e4m3fn).float()
+    v = torch.randint(-8, 9, (batch, Hkv, n, D), generator=g).float()
+    k_scale = torch.full((batch, Hkv, n // blk), 2.0 ** 95)
+    v_scale = torch.full((batch, Hkv, n // blk), 0.25)
+    cache = filled(dims, dtype, fmt, k, v, k_scale, v_scale, blk)
+    q_rot = torch.zeros(batch, G, D)
+    for b, s in enumerate((0.0, 2.0 ** -97, 2.0 ** -99)):
+        q_rot[b, :, 3], q_rot[b, :, 80] = s, -0.75 * s
+    H = Hkv if shared else G
+    sel = [[torch.randperm(n, generator=g)[:rows].tolist() for _ in range(H)] for _ in range(batch)]
+    cos, sin = K.tables(0)
+    got = attend(dims, cache, q_rot.to(dtype), q_rot, sel, 1, shared, 0, cos, sin)
+    for b in range(batch):
+        for h in range(G):
+            at = sel[b][0 if shared else h]
+            kk, vv = k[b, 0, at].double() * 2.0 ** 95, v[b, 0, at].double() * 0.25
+            logit = kk @ q_rot[b, h].double() / D ** 0.5
+            p = logit.softmax(0)
+            # 16 u of the products (two elements: fewer roundings than tests/kv_terms.py counts), 12 u and 6 u a row for the weights
+            d = 16 * K.U * float((kk.abs() @ q_rot[b, h].double().abs()).max()) / D ** 0.5 + (3 * float(logit.abs().max()) + 12 + 6 * rows) * K.U
+            half = 2.0 ** -8 if dtype == torch.bfloat16 else K.U
+            want = p @ vv
+            assert ((got[b, h].double() - want).abs() <= 2 * d * (p @ vv.abs()) * (1 + half) + half * want.abs()).all(), (b, h)
