@@ -13,9 +13,9 @@
 //     terms of a head are added across the columns of a lane row.
 //   - values (A, 16 dimensions x 32 rows) times weights (B).  Logits leave the first product with a head in each column and
 //     four rows of each of two tiles in each lane, which is the B operand of the second as it stands: no exchange between lanes.
-//     Weights are split into bfloat16 terms by truncation, again a column each: the range of float32 stays (v_scale is in the
-//     weight), and 16 bits (8 heads, bfloat16 output) to 24 bits (else) of precision.  A lane loads 8 bytes of each of its
-//     8 rows; the dimensions of tile t are 8 n + t, so that the transposition is a choice of bytes within a lane.
+//     Weights are split into three bfloat16 terms by truncation, again a column each (eight heads have two columns each, and a
+//     second product for the third term): the range of float32 stays (v_scale is in the weight), and its 24 bits.  A lane loads
+//     8 bytes of each of its 8 rows; the dimensions of tile t are 8 n + t, so that the transposition is a choice of bytes within a lane.
 // Window rows are turned back by their distance, (q R_delta) . k = q . (k R_-delta), and go in as two float16 terms.  What is
 // left in the tail, at most a block, is done on the vector ALU.
 // The statistics, all sums and the output are float32.  Logits are kept times log2 e, so that a weight is one exponential.
@@ -258,15 +258,15 @@ __device__ __forceinline__ void pair_weights(const f32x4 (&dot)[2], const PairPl
 }
 
 // The pair's values times its weights.
-template <bool E4M3, int GP, bool EXACT>
+template <bool E4M3, int GP>
 __device__ __forceinline__ void absorb_values(const float (&weight)[8], int term, const PairRows& p, WaveState& st) {
-  // The weights' terms: a column takes its own.
+  // The weights' terms: a column takes its own (eight heads have two columns each: the third term is a product of its own).
   const uint32_t cut1 = term >= 1 ? 0xffff0000u : 0u, cut2 = term >= 2 ? 0xffff0000u : 0u;
   float x[8], rest[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     float y = weight[i];
-    if (GP == 8 && EXACT) {
+    if (GP == 8) {
       const float y1 = y - __uint_as_float(__float_as_uint(y) & 0xffff0000u);
       rest[i] = y1 - __uint_as_float(__float_as_uint(y1) & 0xffff0000u);
     }
@@ -279,7 +279,7 @@ __device__ __forceinline__ void absorb_values(const float (&weight)[8], int term
   for (int i = 0; i < 4; ++i) {
     pw[i] = upper_halves(x[2 * i], x[2 * i + 1]);
     if (GP == 4) pw[i] = term == 3 ? 0u : pw[i];
-    if (GP == 8 && EXACT) rw[i] = term == 0 ? upper_halves(rest[2 * i], rest[2 * i + 1]) : 0u;
+    if (GP == 8) rw[i] = term == 0 ? upper_halves(rest[2 * i], rest[2 * i + 1]) : 0u;
   }
   const bf16x8 pb = __builtin_bit_cast(bf16x8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
 #pragma unroll
@@ -316,7 +316,7 @@ __device__ __forceinline__ void absorb_values(const float (&weight)[8], int term
       }
       const bf16x8 vt = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
       st.o[4 * h + t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pb, st.o[4 * h + t], 0, 0, 0);
-      if (GP == 8 && EXACT) {
+      if (GP == 8) {
         const bf16x8 rb = __builtin_bit_cast(bf16x8, make_uint4(rw[0], rw[1], rw[2], rw[3]));
         st.o[4 * h + t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, rb, st.o[4 * h + t], 0, 0, 0);
       }
@@ -440,7 +440,6 @@ __device__ __forceinline__ f32x4 turned_dot(const uint4 (&k)[2], const float (&c
 // 4 or 8: 16 / GP columns a head.
 template <typename T, bool E4M3, int GP>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_kv8_kernel(AttnArgs a) {
-  constexpr bool EXACT = sizeof(T) == 4;
   __shared__ union {
     struct {
       PairPlaces far[kWaves][2], win[kWaves];
@@ -675,7 +674,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       put_scales(wp, win_place);
       float w[8];
       pair_weights(dot, wp, 0, lrow, st, w);
-      absorb_values<E4M3, GP, EXACT>(w, term, pc, st);
+      absorb_values<E4M3, GP>(w, term, pc, st);
       if (pair + kWaves < n_win) {
         win_place = place_win(pair + kWaves);
         get_scales(win_place);
@@ -705,7 +704,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       dot[1] = fq.dot(p.k[1]);
       float w[8];
       pair_weights(dot, pl, first, lrow, st, w);
-      absorb_values<E4M3, GP, EXACT>(w, term, p, st);
+      absorb_values<E4M3, GP>(w, term, p, st);
     };
     int buf = 0;
 #pragma unroll 1

@@ -75,6 +75,27 @@ def test_weights_have_24_bits(fmt, G, shared, window):
             assert (err <= 8 * 2.0 ** -24 * want.abs()).all(), (b, h, float((err / want.abs().clamp(min=1e-30)).max() * 2 ** 24))
 
 
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+@pytest.mark.parametrize("G, shared", [(4, False), (4, True), (5, True), (8, True)])
+@pytest.mark.parametrize("window", [0, 1])
+def test_weights_next_to_a_border_of_bfloat16(fmt, G, shared, window):
+    """Outputs 2^-18 above and below the middle of two bfloat16 numbers (8 u = 2^-21 is what they may be off by before their rounding):
+    a weight cut to 16 bits rounds the upper one down."""
+    batch, n, blk, Hkv = 2, 16, 16, 1
+    dims = B.make_dims(batch, G, Hkv, D, 16, n, n)
+    v = torch.ones(batch, Hkv, n, D)
+    v[..., ::2] = -1
+    scale = torch.tensor([1 + 2.0 ** -8 + 2.0 ** -18, 1 + 2.0 ** -8 - 2.0 ** -18]).reshape(2, 1, 1)
+    cache = filled(dims, torch.bfloat16, fmt, v, v, scale, scale, blk)
+    zero = torch.zeros(batch, G, D)
+    H = Hkv if shared else G
+    sel = [[[] if window else [3]] * H] * batch
+    cos, sin = K.tables(window)
+    got = attend(dims, cache, zero.bfloat16(), zero, sel, 1, shared, window, cos, sin).double()
+    assert (got[0].abs() == 1 + 2.0 ** -7).all() and (got[1].abs() == 1).all()
+    assert (torch.sign(got) == torch.sign(v[:, :, 3])).all()
+
+
 @pytest.mark.parametrize("G, shared", [(4, False), (4, True), (7, True)])
 @pytest.mark.parametrize("fmt, dtype", [("i8", torch.float32), ("i8", torch.bfloat16), ("e4m3", torch.float32)])
 def test_queries_of_zeros_and_tiny_ones(fmt, dtype, G, shared):
