@@ -46,6 +46,13 @@ typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 
+// Between what some lanes of a wave write to LDS and others of it read, and the other way round: no instruction (a wave's LDS
+// operations are done in order), but what keeps the compiler from moving either past it.
+__device__ __forceinline__ void wave_exchange() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+}
+
 __device__ __forceinline__ float power(float x) { return __builtin_amdgcn_exp2f(x); }
 
 template <int CTRL>
@@ -524,7 +531,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     pc.in = in;
     j = in ? j : 0;   // (a place without a row: the sequence's first one, which has been written and counts for nothing)
     pc.at = block_at(a.cache, b, kv, j >> shift);
+    wave_exchange();
     to.row[lane] = (uint32_t)((pc.at << shift) + (size_t)(j & (blk - 1)));
+    wave_exchange();
     return pc;
   };
   auto get_scales = [&](Place& pc) {
@@ -532,9 +541,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     pc.vs = a.cache.v_scale[pc.at];
   };
   auto put_scales = [&](PairPlaces& to, const Place& pc) {
+    wave_exchange();
     to.ks[lane] = pc.in ? pc.ks : 0.f;
     to.vs[lane] = pc.in ? pc.vs : 0.f;
     to.none[lane] = pc.in ? 0u : ~0u;
+    wave_exchange();
   };
   PairPlaces &wp = s.places.win[wv], *fp = s.places.far[wv];
   auto place_far = [&](PairPlaces& to, int pair) {   // this pair and the next one
@@ -621,6 +632,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       o = rows_sum(o + dpp<0x128>(o));
       if (slot == 0) s_to[to][sub * 16 + e] = o + (again ? s_to[to][sub * 16 + e] * f_old : 0.f);
     }
+    wave_exchange();   // (all lanes have read what the wave stored before)
     if (lane == 0) {
       s_tm[to] = m;
       s_tl[to] = l;
