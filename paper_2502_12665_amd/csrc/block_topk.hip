@@ -393,7 +393,7 @@ __global__ __launch_bounds__(NT) void pick_blocks_kernel(TopkArgs a) {
   __shared__ uint32_t s_band_key[kBandMost];
   __shared__ uint16_t s_band_at[kBandMost];
   __shared__ double2 s_query[MATRIX ? kD : 1];   // of several heads: the sums of their queries and of the magnitudes
-  extern __shared__ uint32_t s_dyn[];   // a bit for each block that is taken out of the band; then the selection
+  extern __shared__ __align__(8) uint32_t s_dyn[];   // a bit for each block that is taken out of the band; then the selection
   // (on the XCD where the head's scores have been written)
   const int of = a.shared ? 1 : a.group;
   int prob, head_of;

@@ -81,7 +81,7 @@ __global__ __launch_bounds__(NW * 64) void append_kernel(BlockCache m, const T* 
                                                          const int32_t* __restrict__ new_lens, int parts) {
   constexpr int D = kRowBytes, NT = NW * 64, SLAB = NW * kWaveRows;
   __shared__ uint32_t s_big[NW];
-  __shared__ float s_lo[NW][D], s_hi[NW][D];
+  __shared__ __align__(8) float s_lo[NW][D], s_hi[NW][D];
   // workgroups: [b][kv][part][key, value]
   const int of = CODES ? 2 : 1;
   const int what = blockIdx.x % of, rest = blockIdx.x / of, part = rest % parts, bh = rest / parts;

@@ -186,7 +186,7 @@ struct PairRows {
   uint2 v[8];
 };
 // Where the rows of two pairs are in the cache, their scales, and 0 or, for a place without a row, all bits: of a wave, in LDS.
-struct PairPlaces {
+struct alignas(16) PairPlaces {
   uint32_t row[2 * kPair];
   float ks[2 * kPair], vs[2 * kPair];
   uint32_t none[2 * kPair];
@@ -447,7 +447,7 @@ __device__ __forceinline__ f32x4 turned_dot(const uint4 (&k)[2], const float (&c
 // 4 or 8: 16 / GP columns a head.
 template <typename T, bool E4M3, int GP>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_kv8_kernel(AttnArgs a) {
-  __shared__ union {
+  __shared__ __align__(16) union {
     struct {
       PairPlaces far[kWaves][2], win[kWaves];
     } places;
