@@ -694,8 +694,10 @@ static int append_impl(const a2ats_dims* d, const a2ats_kv_blocks* blocks, bool 
   if (rc != A2ATS_OK) return rc;
   if (n_new < 0 || n_new > d->ctx_len) return A2ATS_ERR_INVALID_ARG;
   if (n_new == 0) return A2ATS_OK;
+  if (!launchable(*d, d->n_kv_heads, (int64_t)(rows ? 2 : 1) * a2ats::append_parts(n_new, blocks->block),
+                  a2ats::append_threads(blocks->block)))
+    return A2ATS_ERR_UNSUPPORTED;
   if (!k_new || misaligned16(k_new) || (rows && (!v_new || misaligned16(v_new)))) return A2ATS_ERR_INVALID_ARG;
-  if (!launchable(*d, d->n_kv_heads, 2 * a2ats::append_parts(n_new, blocks->block), 512)) return A2ATS_ERR_UNSUPPORTED;
   const hipError_t e = a2ats::launch_append(*d, m, blocks->kv_dtype, blocks->format, rows, k_new, v_new, n_new, seq_lens,
                                             new_lens, (hipStream_t)stream);
   return e == hipSuccess ? A2ATS_OK : A2ATS_ERR_HIP;

@@ -194,6 +194,7 @@ hipError_t launch_codebook_update(const a2ats_dims& d, const float* keys, int n_
 
 // A cache cut into blocks (kv_blocks.hpp): append (codes: the 8-bit rows too, else the bounds alone), selection, attention.
 int append_parts(int n_new, int block);   // workgroups of a sequence and KV head's keys
+int append_threads(int block);            // threads of each
 hipError_t launch_append(const a2ats_dims& d, const BlockCache& m, int kv_dtype, int format, bool codes, const void* k_new,
                          const void* v_new, int n_new, const int32_t* seq_lens, const int32_t* new_lens, hipStream_t stream);
 struct BlockTopkPlan {

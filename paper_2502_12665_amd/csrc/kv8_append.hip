@@ -288,5 +288,6 @@ int append_parts(int n_new, int block) {
   const int slab = append_waves(block) * kWaveRows;
   return (int)(((long)n_new + block - 1 + slab - 1) / slab);
 }
+int append_threads(int block) { return append_waves(block) * 64; }
 
 }  // namespace a2ats
