@@ -540,60 +540,85 @@ def group_shared_step(args, torch, B, synth, wl):
     }))
 
 
+class BlockCacheSteps:
+    """Decode steps of a sequence (batch) over a cache in 8 bits cut into blocks of 16 tokens: all blocks but the last of the workload's
+    ctx_len tokens are appended before, and step i appends token i % tokens of the last one, selects as many blocks as hold top_k
+    tokens, and attends them and the window.  So the incomplete block has one token, two, .. as in generation, the last step
+    completes it, and the step behind that begins the block again."""
+
+    def __init__(self, torch, B, synth, wl, codes, shared, device="cuda"):
+        blk, N = 16, wl.ctx_len
+        self.block, self.first = blk, (N - 1) // blk * blk           # the last block's first token
+        self.tokens = N - self.first
+        x = synth.make_decode_inputs(wl, device=device)
+        self.dims = B.make_dims(wl.batch, wl.n_q_heads, wl.n_kv_heads, wl.head_dim, wl.n_sub, N, self.first + blk)
+        self.cache = B.KvBlocks.empty(self.dims, blk, x["q"].dtype, codes, device=device)
+        self.state = B.BlockDecodeState(self.dims, self.cache, -(-wl.top_k // blk), wl.window, wl.n_sink, x["inv_freq"], wl.wrope_b, shared,
+                                        scores=False)
+        self.q, at = x["q"], self.first
+        self.lens = [torch.full((wl.batch,), at + t + 1, dtype=torch.int32, device=device) for t in range(self.tokens)]
+        self.new = [tuple(x[c][:, :, at + t:at + t + 1].contiguous() for c in ("k", "v")) for t in range(self.tokens)]
+        if at > 0:
+            B.kv8_append(self.dims, self.cache, x["k"][:, :, :at].contiguous(), x["v"][:, :, :at].contiguous(), at,
+                         torch.full((wl.batch,), at, dtype=torch.int32, device=device))
+
+    def step(self, i):
+        t = i % self.tokens
+        return self.state.step(self.q, *self.new[t], self.lens[t])
+
+
 def block_cache_step(args, torch, B, synth, wl):
     """A decode step over a cache in 8 bits cut into blocks of 16 tokens (no codebook): a2ats_kv8_append of the current token,
     a2ats_block_topk of as many blocks as hold the workload's top_k tokens, a2ats_sparse_attn_kv8 over them and the window;
-    with --group-shared one selection per KV head."""
-    blk, N, K, w = 16, wl.ctx_len, wl.top_k, wl.window
-    dims = B.make_dims(wl.batch, wl.n_q_heads, wl.n_kv_heads, wl.head_dim, wl.n_sub, N, (N + blk - 1) // blk * blk)
+    with --group-shared one selection per KV head.  The steps go through the last block's tokens, so the average is over
+    all fills of the incomplete block."""
+    N, K, w = wl.ctx_len, wl.top_k, wl.window
     codes = torch.int8 if args.block_cache == "i8" else torch.float8_e4m3fn
     R = max(1, args.replicas)
-    reps = []
-    for r in range(R):
-        x = synth.make_decode_inputs(wl.replace(seed=wl.seed + r), device="cuda")
-        cache = B.KvBlocks.empty(dims, blk, x["q"].dtype, codes)
-        B.kv8_append(dims, cache, x["k"], x["v"], N)
-        st = B.BlockDecodeState(dims, cache, -(-K // blk), w, wl.n_sink, x["inv_freq"], wl.wrope_b, args.group_shared,
-                                scores=False)
-        reps.append((st, x["q"], x["k"][:, :, -1:].contiguous(), x["v"][:, :, -1:].contiguous()))
-        del x
+    reps = [BlockCacheSteps(torch, B, synth, wl.replace(seed=wl.seed + r), codes, args.group_shared) for r in range(R)]
+    blk, tokens = reps[0].block, reps[0].tokens
+    cycle = R * tokens   # steps after which every cache is where it was
+    done = 0
 
-    def step(i):   # (the last token is appended again: its block is in the tail, and is rounded to the same codes)
-        st, q, k_new, v_new = reps[i % R]
-        st.step(q, k_new, v_new)
+    def steps(n):
+        nonlocal done
+        for i in range(done, done + n):
+            reps[i % R].step(i // R)
+        done += n
 
-    def timed(call, n):
+    def timed(call):
         torch.cuda.synchronize()
         t0 = time.perf_counter()
-        for i in range(n):
-            call(i)
+        call()
         torch.cuda.synchronize()
-        return (time.perf_counter() - t0) * 1e3
+        return (time.perf_counter() - t0) * 1e3 / args.steps
 
-    for i in range(max(args.warmup, R)):
-        step(i)
-    ms_eager = timed(step, args.steps) / args.steps
+    steps(max(args.warmup, R))
+    ms_eager = timed(lambda: steps(args.steps))
     choices = [(ms_eager, "eager")]
-    if not args.no_graph and args.steps % R == 0:
-        big = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(big):
-            for r in range(R):
-                step(r)
-        big.replay()
-        choices.append((timed(lambda i: big.replay(), args.steps // R) / args.steps, f"replay of one hip graph holding {R} steps"))
+    if not args.no_graph and args.steps % cycle == 0:
+        steps(-done % cycle)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            steps(cycle)
+        graph.replay()
+        choices.append((timed(lambda: [graph.replay() for _ in range(args.steps // cycle)]),
+                        f"replays of one hip graph holding {cycle} steps"))
     ms, launch = min(choices)
     heads = wl.n_kv_heads if args.group_shared else wl.n_q_heads
-    bounds_bytes = wl.batch * wl.n_kv_heads * (N // blk) * 2 * wl.head_dim * reps[0][1].element_size()
+    mean = reps[0].first + (tokens + 1) / 2
+    bounds_bytes = wl.batch * wl.n_kv_heads * ((N - w) // blk) * 2 * wl.head_dim * reps[0].q.element_size()
     attn_bytes = wl.batch * heads * (K + w) * 2 * wl.head_dim
     print(json.dumps({
-        "metric": "cached keys/s = B * Hkv * N / time of a WHOLE decode step over an 8-bit cache (append 1 token + block selection + "
+        "metric": "cached keys/s = B * Hkv * tokens / time of a WHOLE decode step over an 8-bit cache (append 1 token + block selection + "
                   "sparse attention)",
-        "value": wl.batch * wl.n_kv_heads * N / (ms * 1e-3), "unit": "keys/s", "n_gpus": 1, "steps": args.steps,
+        "value": wl.batch * wl.n_kv_heads * mean / (ms * 1e-3), "unit": "keys/s", "n_gpus": 1, "steps": args.steps,
         "warmup": args.warmup, "ms_per_step": ms, "launch": launch, "ms_per_step_eager": ms_eager, "higher_is_better": True,
         "scaling": "weak", "vs_baseline": None, "dtype": f"{args.block_cache} K/V, f32 accumulate; {wl.kv_dtype} bounds, f64 decisions",
         "data": "synthetic",
-        "config": {"workload": wl.name, "block": blk, "top_blocks": -(-K // blk), "window": w, "group_shared": args.group_shared,
-                   "replicas_cycled": R},
+        "config": {"workload": wl.name, "tokens": f"{reps[0].first + 1} .. {N}, one more a step, then the last block again", "block": blk,
+                   "top_blocks": -(-K // blk), "window": w, "group_shared": args.group_shared, "replicas_cycled": R},
         "algorithmic_bytes": {"bounds": bounds_bytes, "attended_rows": attn_bytes},
         "GBps": (bounds_bytes + attn_bytes) / (ms * 1e-3) / 1e9}))
 
@@ -714,7 +739,8 @@ def main():
                          "contiguous one; prints a line of its own")
     ap.add_argument("--block-cache", choices=["i8", "e4m3"],
                     help="decode steps over a cache in 8 bits cut into blocks, which bounds of the keys select (with "
-                         "--group-shared: one selection per KV head); prints a line of its own")
+                         "--group-shared: one selection per KV head); prints a line of its own.  In a graph where --steps is a "
+                         "multiple of 16 * --replicas (each cache goes through the 16 fills of its last block)")
     ap.add_argument("--encode-prefill", action="store_true",
                     help="measure the prefill-side key encoder (configuration 5 geometry, 8 of its 32 "
                          "sequences) instead of the decode step, and print its own JSON line")

@@ -448,7 +448,8 @@ typedef struct a2ats_kv_blocks {
  * Append tokens to the cache.  Sequence b has seq_lens[b] (NULL: ctx_len) tokens afterwards; the last m_b of them are
  * new, m_b = new_lens[b] [dev, nullable, int32 B] (NULL: n_new) limited to 0 .. min(n_new, seq_lens[b]): rows 0 .. m_b - 1 of
  *   k_new, v_new [dev, kv_dtype B*Hkv*n_new*D]   pre-RoPE keys, and values
- * A sequence only grows: the tokens before the new ones have been appended by earlier calls.  (It may begin again at 0.)
+ * A sequence only grows: the tokens before the new ones have been appended by earlier calls.  (It may go back to the beginning of a
+ * block, 0 among them: that block's tokens from there on are then the new ones.)
  * A block is rounded when its last token is there, from the values as they were given (its earlier tokens come from the
  * tail), so that the codes do not depend on how the tokens were cut into calls.  With a = max |x| over the block's
  * block * D elements of keys (or of values) of a KV head:
