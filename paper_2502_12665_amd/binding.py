@@ -470,7 +470,7 @@ def _cache_stream(dims: Dims, cache: KvBlocks):
 
 
 def kv8_append(dims: Dims, cache: KvBlocks, k_new, v_new, n_new: int, seq_lens=None, new_lens=None):
-    """Append up to n_new tokens a sequence, k_new / v_new [B, Hkv, n_new, D]; seq_lens count them already."""
+    """Append up to n_new tokens a sequence, k_new / v_new [B, Hkv, n_new, D]; seq_lens count them already, up to dims.ctx_len."""
     B, n = dims.batch, dims.batch * dims.n_kv_heads * n_new * dims.head_dim
     st = _cache_stream(dims, cache)
     rc = lib().a2ats_kv8_append(ctypes.byref(dims), cache.ref, _arg(cache, k_new, "k_new", cache.kv_dtype, n),
@@ -622,7 +622,9 @@ class BlockDecodeState:
         self.ws = torch.empty(n_ws, dtype=torch.uint8, device=dev)
 
     def step(self, q, k_new, v_new, seq_lens=None):
-        """kv8_append of one token a sequence -> block_topk -> sparse_attn_kv8 on the current stream; returns self.out."""
+        """kv8_append of one token a sequence -> block_topk -> sparse_attn_kv8 on the current stream; returns self.out.
+        seq_lens counts that token already and is at most dims.ctx_len (None: ctx_len): a cache is made with room for what it
+        is to hold, a larger length is taken as ctx_len and the token replaces the last one."""
         kv8_append(self.dims, self.cache, k_new, v_new, 1, seq_lens)
         block_topk(self.dims, self.cache, q, self.cos_b, self.sin_b, self.q_rot, self.shared, self.top_blocks, self.window,
                    self.n_sink, seq_lens, self.block_idx, self.block_count, self.block_score, ws=self.ws)

@@ -1,4 +1,7 @@
 """Decode steps over a cache in 8 bits as bench.py times them: the caches hold what was appended, and a step attends it."""
+import os
+import re
+
 import pytest
 import torch
 
@@ -73,3 +76,46 @@ def test_a_sequence_may_go_back_to_the_beginning_of_a_block(fmt, page):
                 assert torch.equal(c.piece(getattr(c.cache, x), b, kv).float().double().reshape(-1, 32, D)[:full], want.codes[x])
                 assert torch.equal(c.piece(getattr(c.cache, x + "_scale"), b, kv).double()[:full], want.scales[x])
                 assert torch.equal(getattr(c.cache, x + "_tail")[b, kv].cpu()[: n - full * 32], getattr(c, x)[b][kv, full * 32:n])
+
+
+def test_the_readme_program():
+    """README.md's code blocks as they stand, behind each other: the tokens that the codes select attended from the 8-bit cache, then 20 generated
+    tokens, after which the cache holds the prompt and all of them."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    code = "\n".join(re.findall(r"```python\n(.*?)```", open(os.path.join(root, "README.md")).read(), re.S))
+    at = code.index("# or blocks selected")
+    env = {}
+    exec(code[:at], env)
+    wl, x, st, cache, grown = (env[n] for n in ("wl", "x", "st", "cache", "grown"))
+    N, w, G = wl.ctx_len, wl.window, wl.n_q_heads // wl.n_kv_heads
+    torch.cuda.synchronize()
+    bs, first = env["bs"], env["out"].cpu()
+    cos_w, sin_w = bs.cos_win.cpu().double(), bs.sin_win.cpu().double()
+
+    def attended(out, h, k, v, q, q_rot, n, positions):
+        s = R.Sequence(k, v, 16, "i8")
+        want, off = R.attend(q.double(), q_rot.double(), s.rows["k"], s.rows["v"], n, positions, w, 0, cos_w, sin_w)
+        err = (out.double() - want).abs()
+        assert (err <= off + 2.0 ** -8 * (want.abs() + off)).all(), (h, float(err.max()))
+        return s
+
+    for h in (0, wl.n_q_heads - 1):
+        assert int(st.topk_count[0, h]) == wl.top_k
+        attended(first[0, h], h, x["k"][0, h // G].cpu(), x["v"][0, h // G].cpu(), x["q"][0, h].cpu(), st.q_rot[0, h].cpu(), N,
+                 st.topk_idx[0, h].tolist())
+    g = gen(1)
+    new = [[torch.randn(1, n, D, generator=g).bfloat16() for n in (wl.n_q_heads, wl.n_kv_heads, wl.n_kv_heads)] for _ in range(20)]
+    env["tokens"] = [(q.cuda(), k.unsqueeze(2).cuda(), v.unsqueeze(2).cuda()) for q, k, v in new]
+    exec(code[at:], env)
+    torch.cuda.synchronize()
+    n = N + 20
+    assert env["seq_lens"].tolist() == [n] and grown.ctx_len >= n
+    for h in (0, wl.n_q_heads - 1):
+        kv = h // G
+        k, v = (torch.cat([x[c][0, kv].cpu()] + [t[i][0, kv:kv + 1] for t in new]) for c, i in (("k", 1), ("v", 2)))
+        blocks = [c for c in bs.block_idx[0, h].tolist() if c >= 0]
+        assert len(blocks) == wl.top_k // 16
+        s = attended(env["out"][0, h].cpu(), h, k, v, new[-1][0][0, h], bs.q_rot[0, h].cpu(), n, R.tokens_of(blocks, n, 16, w, 0))
+        assert R.select(bs.q_rot[0, h:h + 1].cpu().double(), s.bounds, n, 16, w, 0, len(blocks), False)[0][0] == blocks
+        assert torch.equal(cache.k[0, kv].float().cpu().double().reshape(-1, 16, D)[: n // 16], s.codes["k"])
+        assert torch.equal(cache.v_tail[0, kv, : n % 16].cpu(), v[n // 16 * 16:])
