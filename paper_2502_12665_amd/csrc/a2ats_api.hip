@@ -724,13 +724,13 @@ int a2ats_block_topk(const a2ats_dims* d, const a2ats_kv_blocks* blocks, const v
   if (rc != A2ATS_OK) return rc;
   if (top_blocks < 0 || window < 0 || n_sink < 0) return A2ATS_ERR_INVALID_ARG;
   if (top_blocks > 4096) return A2ATS_ERR_UNSUPPORTED;
-  if (!q || !cos_b || !sin_b || !q_rot || !block_count || (top_blocks > 0 && !block_idx)) return A2ATS_ERR_INVALID_ARG;
-  if (top_blocks > 0 && (token_idx == nullptr) != (token_count == nullptr)) return A2ATS_ERR_INVALID_ARG;
-  if (misaligned16(q) || misaligned16(cos_b) || misaligned16(sin_b) || misaligned16(q_rot)) return A2ATS_ERR_INVALID_ARG;
   const a2ats::BlockTopkPlan plan = a2ats::make_block_topk_plan(*d, blocks->block, shared != 0);
   if (!launchable(*d, d->n_kv_heads, plan.chunks, 256) || !launchable(*d, shared ? d->n_kv_heads : d->n_q_heads, 1, 1024))
     return A2ATS_ERR_UNSUPPORTED;
   if (plan.bytes > 0 && (!ws || misaligned16(ws) || ws_bytes < plan.bytes)) return A2ATS_ERR_WORKSPACE;
+  if (!q || !cos_b || !sin_b || !q_rot || !block_count || (top_blocks > 0 && !block_idx)) return A2ATS_ERR_INVALID_ARG;
+  if (top_blocks > 0 && (token_idx == nullptr) != (token_count == nullptr)) return A2ATS_ERR_INVALID_ARG;
+  if (misaligned16(q) || misaligned16(cos_b) || misaligned16(sin_b) || misaligned16(q_rot)) return A2ATS_ERR_INVALID_ARG;
   const hipError_t e = a2ats::launch_block_topk(*d, m, blocks->kv_dtype, q, cos_b, sin_b, q_rot, shared != 0, top_blocks, window,
                                                 n_sink, seq_lens, block_idx, block_count, block_score, token_idx, token_count,
                                                 ws, (hipStream_t)stream);
@@ -749,12 +749,12 @@ int a2ats_sparse_attn_kv8(const a2ats_dims* d, const a2ats_kv_blocks* blocks, co
   if (n_sel < 0 || window < 0 || n_sink < 0) return A2ATS_ERR_INVALID_ARG;
   if (sel_size != 1 && sel_size != blocks->block) return A2ATS_ERR_INVALID_ARG;
   if (n_sel > 4096) return A2ATS_ERR_UNSUPPORTED;
-  if (!q || !q_rot || !sel_count || !out || (n_sel > 0 && !sel_idx)) return A2ATS_ERR_INVALID_ARG;
-  if (window > 0 && (!cos_win || !sin_win)) return A2ATS_ERR_INVALID_ARG;
-  if (misaligned16(q) || misaligned16(q_rot) || misaligned16(cos_win) || misaligned16(sin_win)) return A2ATS_ERR_INVALID_ARG;
   const a2ats::Kv8Plan plan = a2ats::make_kv8_plan(*d, (long)n_sel * sel_size, window, shared != 0);
   if (!launchable(*d, d->n_q_heads, plan.parts, 256)) return A2ATS_ERR_UNSUPPORTED;
   if (plan.bytes > 0 && (!ws || misaligned16(ws) || ws_bytes < plan.bytes)) return A2ATS_ERR_WORKSPACE;
+  if (!q || !q_rot || !sel_count || !out || (n_sel > 0 && !sel_idx)) return A2ATS_ERR_INVALID_ARG;
+  if (window > 0 && (!cos_win || !sin_win)) return A2ATS_ERR_INVALID_ARG;
+  if (misaligned16(q) || misaligned16(q_rot) || misaligned16(cos_win) || misaligned16(sin_win)) return A2ATS_ERR_INVALID_ARG;
   const hipError_t e = a2ats::launch_sparse_attn_kv8(*d, m, blocks->kv_dtype, blocks->format, q, q_rot, sel_idx, sel_count, n_sel,
                                                      log2_of(sel_size), shared != 0, window, n_sink, cos_win, sin_win, seq_lens,
                                                      out, ws, (hipStream_t)stream);

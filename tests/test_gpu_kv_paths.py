@@ -136,3 +136,32 @@ def test_tokens_that_the_codes_select(fmt, heads, kv_heads, shared):
             want, off = R.attend(x["q"][b, h].cpu().double(), st.q_rot[b, h].cpu().double(), s.rows["k"], s.rows["v"], m, pos, w, sink, cos_w, sin_w)
             err = (out[b, h].cpu().double() - want).abs()
             assert (err <= off + 2.0 ** -8 * (want.abs() + off)).all(), (b, h, float(err.max()))
+
+
+@pytest.mark.parametrize("shared, page, dtype, fmt, G", [(False, 0, "f32", "e4m3", 1), (True, 64, "bf16", "i8", 7), (True, 0, "f32", "i8", 5)])
+def test_decode_steps_over_two_borders(shared, page, dtype, fmt, G):
+    """61 tokens, one by one: the sequences complete two blocks each and end inside of one, every eleventh step and those about the borders
+    compared with float64."""
+    c = Case([190 + 61, 61], G, 1, 32, fmt, dtype, page, seed=130)
+    c.append([190, 0])
+    st = B.BlockDecodeState(c.dims, c.cache, 3, 20, 2, c.inv, 2048, shared)
+    lens = torch.tensor([190, 0], dtype=torch.int32, device="cuda")
+    steps = completed = checked = 0
+    for i in range(61):
+        lens += 1
+        k, v = (torch.stack([t[b][:, (190, 0)[b] + i] for b in range(2)]).unsqueeze(2).contiguous().cuda() for t in (c.k, c.v))
+        q = torch.randn(2, G, D, generator=gen(1000 + i)).to(c.dtype)
+        out = st.step(q.cuda(), k, v, lens)
+        c.have = [190 + i + 1, i + 1]
+        steps += 1
+        completed += sum(n % 32 == 0 for n in c.have)
+        if i % 11 == 0 or any(n % 32 in (0, 1) for n in c.have):
+            checked += 1
+            c.q = q
+            torch.cuda.synchronize()
+            c.check_cache()
+            o = {"q_rot": st.q_rot.cpu(), "idx": st.block_idx.cpu(), "count": st.block_count.cpu(), "score": st.block_score.cpu()}
+            check_select(c, o, shared, 3, 20, 2)
+            sel = [[[j for j in o["idx"][b, h].tolist() if j >= 0] for h in range(1 if shared else G)] for b in range(2)]
+            check_attend(c, out.cpu(), o["q_rot"], st.cos_win.cpu().double(), st.sin_win.cpu().double(), sel, 32, shared, 20, 2)
+    assert lens.tolist() == [251, 61] and (steps, completed) == (61, 3) and checked == 11
