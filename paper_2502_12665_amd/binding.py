@@ -379,21 +379,14 @@ class KvBlocks:
             raise ValueError("k, v, their scales and tails are given together")
         if k is None and bounds is None:
             raise ValueError("neither rows nor bounds")
-        if kv_dtype not in (torch.float32, torch.bfloat16):
-            raise TypeError(f"unsupported dtype {kv_dtype}")
-        if block not in (16, 32, 64, 128):
-            raise ValueError("block is 16, 32, 64 or 128")
+        _check_blocks(dims, block, kv_dtype, page_table, page_size)
         B, Hkv, D = dims.batch, dims.n_kv_heads, dims.head_dim
         if page_table is not None:
-            if page_size < block or page_size & (page_size - 1):
-                raise ValueError("page_size is a power of two of at least a block")
             some = k if k is not None else bounds
             lead = (some.shape[0], Hkv)
             slots = page_size
             _check_tensor(page_table, "page_table", torch.int32, (B, -(-dims.ctx_stride // page_size)))
         else:
-            if dims.ctx_stride % block:
-                raise ValueError("ctx_stride is a multiple of block")
             lead, slots = (B, Hkv), int(dims.ctx_stride)
         self.format = I8
         if k is not None:
@@ -424,6 +417,7 @@ class KvBlocks:
     def empty(cls, dims: Dims, block: int, kv_dtype: torch.dtype, codes: Optional[torch.dtype] = torch.int8, bounds: bool = True,
               page_table=None, page_size: int = 0, n_pages: int = 0, device="cuda"):
         """A cache in new memory (scales zero).  codes None: only the bounds."""
+        _check_blocks(dims, block, kv_dtype, page_table, page_size)
         B, Hkv, D = dims.batch, dims.n_kv_heads, dims.head_dim
         lead, slots = ((n_pages, Hkv), page_size) if page_table is not None else ((B, Hkv), int(dims.ctx_stride))
         t = {}
@@ -435,6 +429,18 @@ class KvBlocks:
         if bounds:
             t["bounds"] = torch.empty(lead + (slots // block, 2, D), dtype=kv_dtype, device=device)
         return cls(dims, block, kv_dtype, page_table=page_table, page_size=page_size, **t)
+
+
+def _check_blocks(dims: Dims, block: int, kv_dtype: torch.dtype, page_table, page_size: int):
+    if kv_dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"unsupported dtype {kv_dtype}")
+    if block not in (16, 32, 64, 128):
+        raise ValueError("block is 16, 32, 64 or 128")
+    if page_table is None:
+        if dims.ctx_stride % block:
+            raise ValueError("ctx_stride is a multiple of block")
+    elif page_size < block or page_size & (page_size - 1):
+        raise ValueError("page_size is a power of two of at least a block")
 
 
 def _check_tensor(t: torch.Tensor, name: str, dtype: torch.dtype, shape):

@@ -4,6 +4,7 @@ queries without an address."""
 import ctypes
 
 import pytest
+import torch
 
 ONE = 16
 
@@ -91,3 +92,15 @@ def test_the_workspace_figure_of_attention(B, batch, heads, kv_heads, n, window)
                 most = max(most, need)
         assert most == figure
     assert parts <= {0} | set(range(2, 13))
+
+
+def test_caches_of_blocks_that_there_are_not(B):
+    """Refused before anything is allocated."""
+    d = B.make_dims(2, 4, 2, 128, 16, 100, 128)
+    table = torch.zeros(2, 4, dtype=torch.int32)
+    for kw, err in ((dict(block=0), ValueError), (dict(block=24), ValueError), (dict(block=256), ValueError), (dict(kv_dtype=torch.float16), TypeError),
+                    (dict(page_table=table, page_size=0, n_pages=8), ValueError), (dict(page_table=table, page_size=48, n_pages=8), ValueError)):
+        with pytest.raises(err):
+            B.KvBlocks.empty(d, **{"block": 32, "kv_dtype": torch.bfloat16, "device": "nowhere", **kw})
+    with pytest.raises(ValueError):
+        B.KvBlocks.empty(B.make_dims(2, 4, 2, 128, 16, 100, 100), 16, torch.bfloat16, device="nowhere")
