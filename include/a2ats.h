@@ -503,7 +503,10 @@ int a2ats_block_topk(const a2ats_dims* dims, const a2ats_kv_blocks* blocks, cons
  *     sel_size 1: tokens, as a2ats_score_topk gives them;  sel_size == block: blocks, of which the candidate tokens are attended
  *   shared 0: of each query head, H = Hq;  otherwise of each KV head, H = Hkv, attended by its G heads.
  * Indices may be in any order but not repeat; what is not a candidate, [sink_end, n - window), is not attended.
- * Rows of complete blocks are code * scale, those of the incomplete block are in the tails.  float32 accumulation; out
+ * Rows of complete blocks are code * scale, those of the incomplete block are in the tails.  Products, sums and weights are those of
+ * float32 (weights and e4m3 and int8 codes enter their products whole; turned window keys and, for 5 to 8 heads of a shared
+ * selection, queries as two float16 numbers, off by at most 2^-23 of each element; of an int8 key's query what is below 2^-30 of its
+ * largest element is cut); a key's scale multiplies the product with its codes, which has to be a float32 itself.  out
  * [dev, out, kv_dtype B*Hq*D] is rounded once (zeros where nothing is attended, else NaN for a head whose query is not
  * finite).  q, q_rot, cos_win, sin_win as in
  * a2ats_sparse_attn (all 16-byte aligned); `bounds` is not read.

@@ -14,8 +14,9 @@
 //
 // Measured: 8 KV heads x 32768 tokens, bfloat16 to int8 with bounds, 49 us = 4.2 TB/s of 206 MB, of which the bounds' minima and
 // maxima (vector ALU) are 8; e4m3 without bounds runs at the rate of a large copy (4.9 TB/s).  4 x 4 x 4099 tokens, float32 to
-// e4m3 in pages, 13.6 - 15 us = 3.4 - 3.8 TB/s.  One token of 16 x 8 heads: 4.7 us, of which an empty launch is 1.6; the rest are the
-// requests that wait for each other (length, rows, bounds).  Requesting the bounds and the tail's rows ahead of the barrier did
+// e4m3 in pages, 13.6 - 15 us = 3.4 - 3.8 TB/s.  Bounds alone, 8 KV heads x 32768 tokens: bfloat16 20.7 us = 3.4 TB/s (the minima and
+// maxima), float32 29.7 us = 4.8 TB/s.  One token of 16 x 8 heads: 4.7 us (bounds alone 3.5), of which an empty launch is 1.6; the rest are
+// the requests that wait for each other (length, rows, bounds).  Requesting the bounds and the tail's rows ahead of the barrier did
 // not shorten it (4.9).
 #include "internal.hpp"
 #include "kv_blocks.hpp"

@@ -9,22 +9,25 @@
 // the precision of the float32 operand:
 //   - keys (A, 16 rows x 128) times queries (B).  A column is (head, term): int8 keys go into v_mfma_i32_16x16x64_i8 as they
 //     come from memory, the query as four signed digits to the base 256 of q * 2^(30 - e), |q| < 2^e, so that each digit's product
-//     is an exact integer; e4m3 keys become float16 (exact) and the query three float16 terms (eight heads: two, 22 bits).  The
-//     terms of a head are added across the columns of a lane row.
+//     is an exact integer; e4m3 keys become float16 (exact) and the query three float16 terms (eight heads: two, to the
+//     nearest each: off by at most 2^-23 of an element, as two roundings of float32, with no sign of its own).  The terms of a head
+//     are added across the columns of a lane row.
 //   - values (A, 16 dimensions x 32 rows) times weights (B).  Logits leave the first product with a head in each column and
 //     four rows of each of two tiles in each lane, which is the B operand of the second as it stands: no exchange between lanes.
 //     Weights are split into three bfloat16 terms by truncation, again a column each (eight heads have two columns each, and a
 //     second product for the third term): the range of float32 stays (v_scale is in the weight), and its 24 bits.  A lane loads
 //     8 bytes of each of its 8 rows; the dimensions of tile t are 8 n + t, so that the transposition is a choice of bytes within a lane.
-// Window rows are turned back by their distance, (q R_delta) . k = q . (k R_-delta), and go in as two float16 terms.  What is
-// left in the tail, at most a block, is done on the vector ALU.
+// Window rows are turned back by their distance, (q R_delta) . k = q . (k R_-delta), and go in as two float16 terms (2^-23, as
+// above; a third would be half as many products again).  What is left in the tail, at most a block, is done on the vector ALU.
 // The statistics, all sums and the output are float32.  Logits are kept times log2 e, so that a weight is one exponential.
 //
-// Measured: 32 x 28 heads of 2176 rows, e4m3, 97 - 101 us = 4.9 - 5.1 TB/s of 497 MB (the rate of a large copy); the same rows of int8
-// 91 us; 4 x 32 heads of 2304 rows, int8, in 4 parts 21 us = 3.4 TB/s with the merge of 2.5; one selection for 4 heads, 16 x 8 of
-// 1152 rows in pages, in 2 parts 20.5 us = 1.9 TB/s: few rows, and requests that wait for each other (length and index, page, row),
-// of which a wave has two pairs of rows in flight.  More in flight does not fit: 128 registers for four waves a SIMD spill, and
-// a spill waits for all loads (three times slower), so there are two waves a SIMD with 256.
+// Measured: 32 x 28 heads of 2176 rows, e4m3, 97 - 101 us for 497 MB of rows that heads ask for, of which 453 MB are different ones (the
+// heads of a KV head share the rest in L2): 4.5 - 4.7 TB/s, a large copy has 4.9; the same rows of int8, in blocks of 16, 93 us; 4 x 32
+// heads of 2304 rows, int8, in 4 parts 21 us = 3.4 TB/s, of which the merge is 4; one selection for 4 heads, 16 x 8 of
+// 1152 rows in pages, in 2 parts 20.5 us = 1.9 TB/s, for 7 heads, 32 x 4 of 2176 rows in 4 parts, int8 24, e4m3 23 us = 3.1 TB/s (float32
+// queries the same within 4 %): few rows, and requests that wait for each other (length and index, page, row), of which a wave has two
+// pairs of rows in flight.  More in flight does not fit: 128 registers for four waves a SIMD spill, and a spill waits for all
+// loads (three times slower), so there are two waves a SIMD with 256.
 #include <algorithm>
 #include <cfloat>
 
@@ -145,7 +148,7 @@ __device__ __forceinline__ int row_exponent(const float (&x)[32], bool& ok) {
 }
 
 // A query as float16 terms, for the columns of the first three (eight heads: two): x = 2^(e - 8) (t0 + t1 + t2) but for 2^-33 of 2^e
-// (half the least float16; eight heads: 2^-22).  Returns 2^(e - 8).
+// (half the least float16) and, for eight heads, 2^-23 of x.  Returns 2^(e - 8).
 template <int GP>
 __device__ __forceinline__ float query_terms(const float (&x)[32], int term, bool active, f16x8 (&q)[4]) {
   bool ok;
@@ -861,7 +864,7 @@ __global__ __launch_bounds__(kD) void attn_kv8_merge_kernel(const float* __restr
 
 }  // namespace
 
-// Parts: a second launch (2.5 us) and as many more first requests to wait for, against rows that wait for each other.  From all
+// Parts: a second launch (3 to 4.6 us in whole steps, 2 at least) and as many more first requests to wait for, against rows that wait for each other.  From all
 // counts of parts up to 32 of 2 to 896 problems with 160 to 2304 rows (bfloat16, int8, selections of one head and shared by four), us
 // with one part -> with the parts taken:
 //   - a workgroup for every CU where there are few problems: 4 problems, 576 rows 10.4 -> 8.4 (8 parts), 2304 rows 27.0 -> 9.9
