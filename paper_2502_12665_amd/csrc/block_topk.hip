@@ -24,8 +24,9 @@
 // each: scores 27.7 us = 4.85 TB/s of 134 MB (the rate of a large copy), selection 11 (a chain of a dozen phases of 0.5 to 2 us:
 // range, one digit, band, its exact scores, ranks, output).  float32 bounds, scores: 4 x 8 KV heads of 4096 blocks, 4 heads each,
 // 34.5 us = 3.9 TB/s of 134 MB; 8 x 4 of 2048, one selection for 7 heads 17.3 = 3.9 TB/s, 7 heads 20.4, 4 x 8 of 2048 with 8 heads
-// 21.6 = 3.1 TB/s (from 7 heads on two waves a SIMD, 180 and 202 registers); selections 5 to 7.  Selecting in the last of a head's score workgroups, one launch
-// for both, was slower: its phases do not overlap the stream of the others by as much as they then cost.
+// 21.6 = 3.1 TB/s (from 7 heads on two waves a SIMD, 180 and 202 registers); selections 5 to 7.
+// Selecting in the last of a head's score workgroups, one launch for both, was slower: its phases do not overlap the stream of
+// the others by as much as they then cost.
 #include <algorithm>
 
 #include "internal.hpp"

@@ -52,6 +52,29 @@ def test_shared_rows_of_the_incomplete_block_in_parts(heads, kv_heads, n_sel):
     check_attend(c, *got, sel, 1, True, 11, 5)
 
 
+@pytest.mark.parametrize("fmt, dtype", [("i8", "f32"), ("i8", "bf16"), ("e4m3", "f32"), ("e4m3", "bf16")])
+@pytest.mark.parametrize("G", [2, 4, 5, 8])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_one_head_of_a_shared_selection_that_is_not_finite(fmt, dtype, G, bad):
+    """Its output is NaN; those of the heads that share its tile are what they are without it, bit for bit: far rows, window, tail."""
+    c = Case([190, 96], 2 * G, 2, 32, fmt, dtype, seed=140 + G, bounds=False)
+    c.append(c.lens)
+    sel = draw_sel(c, 32, True, 3, 40, 1, 141)
+    fine, q_rot = run_attend(c, sel, 32, True, 40, 1)[:2]
+    wrong, q = q_rot.clone(), c.q.clone()
+    wrong[0, 1, 77] = bad                                  # (far rows of one head, the window of another)
+    c.q[1, G, 3] = bad
+    got = run_attend(c, sel, 32, True, 40, 1, q_rot=wrong)[0]
+    assert got[0, 1].isnan().all() and got[1, G].isnan().all()
+    keep = torch.ones(2, 2 * G, dtype=torch.bool)
+    keep[0, 1] = keep[1, G] = False
+    assert torch.equal(got[keep], fine[keep])
+    c.q = q
+    # nothing but placeholders for a head that is not finite: zeros
+    none = [[[], []], [[], []]]
+    assert (run_attend(c, none, 32, True, 0, 0, q_rot=wrong)[0] == 0).all()
+
+
 @pytest.mark.parametrize("blocks", [255, 256, 257, 1024, 1025, 2047, 2048, 2049, 3000, 4096])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_selection_on_either_side_of_its_kernels_borders(blocks, dtype):
