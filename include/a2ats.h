@@ -84,7 +84,7 @@ enum { A2ATS_F32 = 0, A2ATS_BF16 = 1 };                       /* element types o
 enum { A2ATS_W_NONE = 0, A2ATS_W_DIAG = 1, A2ATS_W_BLOCK = 2 }; /* encoder distortion              */
 enum { A2ATS_W_PREPARED = 0x100 };   /* flag for weight_mode, see a2ats_encode_prepare */
 enum { A2ATS_OP_ENCODE = 0, A2ATS_OP_LUT = 1, A2ATS_OP_SCORE_TOPK = 2, A2ATS_OP_ATTN = 3, A2ATS_OP_FIT = 4,
-       A2ATS_OP_SEED = 5, A2ATS_OP_BLOCK_TOPK = 6, A2ATS_OP_ATTN_KV8 = 7 };
+       A2ATS_OP_SEED = 5, A2ATS_OP_BLOCK_TOPK = 6, A2ATS_OP_ATTN_KV8 = 7, A2ATS_OP_ATTN_KV4 = 8 };
 enum { A2ATS_I8 = 0, A2ATS_E4M3 = 1 };   /* formats of a cache held in 8 bits, see a2ats_kv8_append */
 
 int a2ats_version(void);
@@ -97,7 +97,7 @@ size_t a2ats_lut_elems(const a2ats_dims* dims);
  * A2ATS_OP_ATTN and A2ATS_OP_SCORE_TOPK the figure covers every call with up to 64 sink tokens; a
  * call with more may need more and is refused with A2ATS_ERR_WORKSPACE if `ws` is too small. */
 size_t a2ats_workspace_bytes(const a2ats_dims* dims, int op, int32_t top_k, int32_t window);
-/* (A2ATS_OP_BLOCK_TOPK: covers every block size and both kinds of selection.  A2ATS_OP_ATTN_KV8: `top_k` is the number of
+/* (A2ATS_OP_BLOCK_TOPK: covers every block size and both kinds of selection.  A2ATS_OP_ATTN_KV8 and A2ATS_OP_ATTN_KV4: `top_k` is the number of
  * selected tokens, n_sel * sel_size; both kinds of selection and any number of sinks.) */
 
 /*
@@ -516,6 +516,84 @@ int a2ats_sparse_attn_kv8(const a2ats_dims* dims, const a2ats_kv_blocks* blocks,
                           const int32_t* sel_idx, const int32_t* sel_count, int32_t n_sel, int32_t sel_size, int32_t shared,
                           int32_t window, int32_t n_sink, const float* cos_win, const float* sin_win,
                           const int32_t* seq_lens, void* out, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * A key/value cache held in 4 bits: e2m1 numbers (0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives, code 0 .. 7 and a sign in bit 3)
+ * with a scale, a power of two, for each group of 32 dimensions of a token's key and of its value.  136 bytes a token and KV head,
+ * about half of a cache in 8 bits; a token is rounded by itself, when it comes, so that there are no tails.
+ * A token's row is 128 bytes: 64 of its key's codes, byte i with dimensions 2 i (low half) and 2 i + 1 (high half); 64 of its
+ * value's, byte 4 n + g with dimensions 32 g + 2 n and 32 g + 2 n + 1, g < 4, n < 16.  Its scales are 8 bytes, exponents + 127 (0 for
+ * a group of zeros, 255 for NaN): the key's groups 0 .. 3, then the value's.
+ * Blocks, "piece" and pages are as in a2ats_kv_blocks; they say where rows are, which tokens a selected block has and what the
+ * bounds are about, and nothing about the rounding.  rows: 16-byte aligned, scales: 8, bounds: 16, the page table: 4.
+ */
+typedef struct a2ats_kv4 {
+  void* rows;                 /* [dev, u8 piece * block * 128]                                          */
+  void* scales;               /* [dev, u8 piece * block * 8]                                            */
+  void* bounds;               /* [dev, nullable, kv_dtype piece * 2 * D] as in a2ats_kv_blocks           */
+  const int32_t* page_table;
+  int32_t page_size;
+  int32_t block;
+  int32_t kv_dtype;           /* of keys, values, queries, outputs and bounds                            */
+} a2ats_kv4;
+
+/*
+ * Append tokens.  seq_lens, new_lens, n_new, k_new and v_new are as in a2ats_kv8_append: sequence b has seq_lens[b] tokens
+ * afterwards, the last m_b of them are rows 0 .. m_b - 1 of k_new / v_new.  Which tokens come in which call does not matter, and
+ * tokens may be written again (with bounds: from the beginning of a block on; otherwise they stay bounds of what was there too).
+ * With a = max |x| over a group: scale 2^e, the least power of two with a <= 6 * 2^e; codes x / 2^e rounded to the nearest
+ * e2m1 number, ties to even, as for real numbers, with the sign of x.  a < 2^-100: scale byte 0 and codes 0.  A group with an element that is not finite, or a >=
+ * 2^127: scale NaN and codes 0, so that what attends it is NaN (of a value: in that group's dimensions).
+ * bounds (if not NULL) are those of the keys as given, as in a2ats_kv8_append.  Nothing else is written.  n_new == 0 is a no-op.
+ */
+int a2ats_kv4_append(const a2ats_dims* dims, const a2ats_kv4* cache, const void* k_new, const void* v_new, int32_t n_new,
+                     const int32_t* seq_lens, const int32_t* new_lens, void* stream);
+
+/*
+ * Read back what a2ats_kv4_append with the same lengths has written: the last m_b = min(new_lens[b], n_rows, seq_lens[b]) tokens
+ * before seq_lens[b] (new_lens NULL: n_rows), as rows 0 .. m_b - 1 of
+ *   k_out, v_out [dev, out, out_dtype B*Hkv*n_rows*D, 16-byte aligned; either may be NULL, not both]
+ * code * scale exactly, in either type.  Later rows are left as they are.  (All of a cache: n_rows = ctx_len.  float32 keys
+ * of one call are what a2ats_encode_keys takes.)  n_rows == 0 is a no-op, n_rows <= ctx_len.  `bounds` and kv_dtype are not used.
+ */
+int a2ats_kv4_read(const a2ats_dims* dims, const a2ats_kv4* cache, int32_t n_rows, const int32_t* seq_lens, const int32_t* new_lens,
+                   void* k_out, void* v_out, int out_dtype, void* stream);
+
+/*
+ * a2ats_sparse_attn_kv8 over a cache in 4 bits: arguments, attended set and results as there, every row code * scale.  Products,
+ * sums and weights are those of float32 (queries, weights and far keys enter their products whole; turned window keys as two float16 numbers, off by at
+ * most 2^-23 of each element and 2^-26 of the row's largest, and for 5 to 8 heads of a shared selection the queries of window rows likewise).  The block selection over such a cache is
+ * a2ats_block_topk, given its bounds, block, kv_dtype, page_table and page_size in an a2ats_kv_blocks.
+ * Workspace: a2ats_workspace_bytes(dims, A2ATS_OP_ATTN_KV4, n_sel * sel_size, window).
+ */
+int a2ats_sparse_attn_kv4(const a2ats_dims* dims, const a2ats_kv4* cache, const void* q, const float* q_rot, const int32_t* sel_idx,
+                          const int32_t* sel_count, int32_t n_sel, int32_t sel_size, int32_t shared, int32_t window, int32_t n_sink,
+                          const float* cos_win, const float* sin_win, const int32_t* seq_lens, void* out, void* ws, size_t ws_bytes,
+                          void* stream);
+
+/*
+ * Norms of queries and keys for each head, for models that have them (between the projections and the rotation), and the
+ * rotation by the tokens' own positions, in one pass over the new tokens:
+ *     y = x w / sqrt(mean(x^2) + eps),    y R_p,
+ * x the D elements of a head of a token, p the token's position.  Of sequence b, rows t < m_b of n_new are tokens, at positions
+ * seq_lens[b] - m_b + t (m_b as in a2ats_kv8_append); rows after them are neither read nor written.
+ *   q, k               [dev, dtype] element (b, t, head, d) at (b * n_new + t) * stride + head * D + d, the layout of the
+ *                      projections; stride (of elements, a multiple of 8) >= Hq*D / Hkv*D, so that both may be parts of one tensor.
+ *                      Either may be NULL: then it has no outputs.
+ *   q_weight, k_weight [dev, nullable, f32 D]   w; NULL: ones.  eps: 2^-126 <= eps <= 1
+ *   cos_pos, sin_pos   [dev, f32 n_pos*D/2]     rows p < n_pos of a2ats_rope_tables (its cos_win / sin_win), n_pos >= ctx_len; NULL if
+ *                                               neither q_pos nor k_pos is asked for
+ *   q_norm, k_norm     [dev, out, nullable, dtype B*H*n_new*D]   y: queries and keys of a decode step (a2ats_build_lut, a2ats_block_topk,
+ *                                               attention) and keys to be cached (a2ats_kv4_append, a2ats_kv8_append) are not rotated
+ *   q_pos, k_pos       [dev, out, nullable, dtype B*H*n_new*D]   y R_p: for the prompt's own attention
+ * At least one output; outputs do not overlap inputs or each other.  Float32 arithmetic, each output rounded once; no square
+ * overflows.  A row with an element that is not finite is not finite either: NaN where that element is infinite (or in all of the row, for a NaN).
+ * All pointers 16-byte aligned but for the lengths (4).  n_new == 0 is a no-op, n_new <= ctx_len.  No workspace.
+ */
+int a2ats_qk_norm_rope(const a2ats_dims* dims, const void* q, int64_t q_stride, const void* k, int64_t k_stride, int dtype,
+                       int32_t n_new, const float* q_weight, const float* k_weight, float eps, const float* cos_pos,
+                       const float* sin_pos, int32_t n_pos, const int32_t* seq_lens, const int32_t* new_lens, void* q_norm,
+                       void* k_norm, void* q_pos, void* k_pos, void* stream);
 
 /*
  * Offline codebook construction (paper section 4.2).

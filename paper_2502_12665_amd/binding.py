@@ -18,7 +18,7 @@ LIB_PATH = os.path.join(_HERE, "liba2ats.so")
 F32, BF16 = 0, 1
 W_NONE, W_DIAG, W_BLOCK = 0, 1, 2
 W_PREPARED = 0x100
-OP_ENCODE, OP_LUT, OP_SCORE_TOPK, OP_ATTN, OP_FIT, OP_SEED, OP_BLOCK_TOPK, OP_ATTN_KV8 = 0, 1, 2, 3, 4, 5, 6, 7
+OP_ENCODE, OP_LUT, OP_SCORE_TOPK, OP_ATTN, OP_FIT, OP_SEED, OP_BLOCK_TOPK, OP_ATTN_KV8, OP_ATTN_KV4 = 0, 1, 2, 3, 4, 5, 6, 7, 8
 I8, E4M3 = 0, 1
 EXPORTS = ["a2ats_version", "a2ats_status_string", "a2ats_lut_elems", "a2ats_workspace_bytes", "a2ats_encode_prepare",
            "a2ats_rope_tables", "a2ats_encode_keys", "a2ats_build_lut", "a2ats_score_topk",
@@ -28,7 +28,7 @@ EXPORTS = ["a2ats_version", "a2ats_status_string", "a2ats_lut_elems", "a2ats_wor
            "a2ats_second_moment", "a2ats_codebook_update", "a2ats_kmeanspp_seed", "a2ats_sparse_attn_paged",
            "a2ats_sparse_attn_static", "a2ats_score_topk_paged", "a2ats_codes_to_pages",
            "a2ats_sparse_attn_host", "a2ats_kv8_append", "a2ats_key_bounds", "a2ats_block_topk",
-           "a2ats_sparse_attn_kv8"]
+           "a2ats_sparse_attn_kv8", "a2ats_kv4_append", "a2ats_kv4_read", "a2ats_sparse_attn_kv4", "a2ats_qk_norm_rope"]
 
 
 class A2atsError(RuntimeError):
@@ -46,6 +46,11 @@ class Dims(ctypes.Structure):
 class KvBlocksStruct(ctypes.Structure):
     _fields_ = [(x, ctypes.c_void_p) for x in ("k", "v", "k_scale", "v_scale", "k_tail", "v_tail", "bounds", "page_table")] + \
                [(x, ctypes.c_int32) for x in ("page_size", "block", "format", "kv_dtype")]
+
+
+class Kv4Struct(ctypes.Structure):
+    _fields_ = [(x, ctypes.c_void_p) for x in ("rows", "scales", "bounds", "page_table")] + \
+               [(x, ctypes.c_int32) for x in ("page_size", "block", "kv_dtype")]
 
 
 _lib = None
@@ -120,6 +125,16 @@ def lib() -> ctypes.CDLL:
         L.a2ats_block_topk.argtypes = [dp, bp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.a2ats_sparse_attn_kv8.restype = ctypes.c_int
         L.a2ats_sparse_attn_kv8.argtypes = [dp, bp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+        fp = ctypes.POINTER(Kv4Struct)
+        L.a2ats_kv4_append.restype = ctypes.c_int
+        L.a2ats_kv4_append.argtypes = [dp, fp, vp, vp, i32, vp, vp, vp]
+        L.a2ats_kv4_read.restype = ctypes.c_int
+        L.a2ats_kv4_read.argtypes = [dp, fp, i32, vp, vp, vp, vp, ctypes.c_int, vp]
+        L.a2ats_sparse_attn_kv4.restype = ctypes.c_int
+        L.a2ats_sparse_attn_kv4.argtypes = [dp, fp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.a2ats_qk_norm_rope.restype = ctypes.c_int
+        L.a2ats_qk_norm_rope.argtypes = [dp, vp, ctypes.c_int64, vp, ctypes.c_int64, ctypes.c_int, i32, vp, vp, ctypes.c_float,
+                                         vp, vp, i32, vp, vp, vp, vp, vp, vp, vp]
         _lib = L
     return _lib
 
@@ -534,6 +549,153 @@ def sparse_attn_kv8(dims: Dims, cache: KvBlocks, q, q_rot, sel_idx, sel_count, n
     _check(rc, "a2ats_sparse_attn_kv8")
 
 
+class Kv4Cache:
+    """A key/value cache held in 4 bits (a2ats_kv4): the tensors and their description, nothing else.
+
+    rows      uint8 [B, Hkv, ctx_stride, 128], or pages [pages, Hkv, page_size, 128]: a token's codes, key then value
+    scales    uint8 [.., 8]: the exponents of its eight groups
+    bounds    kv_dtype [.., ctx_stride / block, 2, D] (pages: page_size / block), or None
+    blocks is the KvBlocks of the bounds alone, which key_bounds and block_topk take (None without bounds)."""
+
+    def __init__(self, dims: Dims, block: int, kv_dtype: torch.dtype, rows, scales, bounds=None, page_table=None, page_size: int = 0):
+        _check_blocks(dims, block, kv_dtype, page_table, page_size)
+        B, Hkv = dims.batch, dims.n_kv_heads
+        if page_table is not None:
+            lead, slots = (rows.shape[0], Hkv), page_size
+            _check_tensor(page_table, "page_table", torch.int32, (B, -(-dims.ctx_stride // page_size)))
+        else:
+            lead, slots = (B, Hkv), int(dims.ctx_stride)
+        _check_tensor(rows, "rows", torch.uint8, lead + (slots, 128))
+        _check_tensor(scales, "scales", torch.uint8, lead + (slots, 8))
+        if bounds is not None and bounds.shape[0] != lead[0]:
+            raise ValueError("bounds and rows have different pages")
+        for t in (scales, bounds, page_table):
+            if t is not None and t.device != rows.device:
+                raise ValueError("the tensors of a cache are on one device")
+        self.blocks = None if bounds is None else KvBlocks(dims, block, kv_dtype, bounds=bounds, page_table=page_table, page_size=page_size)
+        self.block, self.kv_dtype, self.page_size, self.page_table = block, kv_dtype, page_size, page_table
+        self.rows, self.scales, self.bounds = rows, scales, bounds
+        self.device, self.device_index = rows.device, rows.get_device()
+        p = [None if t is None else t.data_ptr() for t in (rows, scales, bounds, page_table)]
+        self.struct = Kv4Struct(*p, page_size, block, F32 if kv_dtype == torch.float32 else BF16)
+        self.ref = ctypes.byref(self.struct)
+        self.batch, self.n_kv_heads, self.ctx_stride = B, Hkv, int(dims.ctx_stride)
+
+    @classmethod
+    def empty(cls, dims: Dims, block: int, kv_dtype: torch.dtype, bounds: bool = True, page_table=None, page_size: int = 0,
+              n_pages: int = 0, device="cuda"):
+        """A cache in new memory (zeros)."""
+        _check_blocks(dims, block, kv_dtype, page_table, page_size)
+        lead = (n_pages, dims.n_kv_heads) if page_table is not None else (dims.batch, dims.n_kv_heads)
+        slots = page_size if page_table is not None else int(dims.ctx_stride)
+        rows = torch.zeros(lead + (slots, 128), dtype=torch.uint8, device=device)
+        scales = torch.zeros(lead + (slots, 8), dtype=torch.uint8, device=device)
+        bd = torch.empty(lead + (slots // block, 2, dims.head_dim), dtype=kv_dtype, device=device) if bounds else None
+        return cls(dims, block, kv_dtype, rows, scales, bd, page_table, page_size)
+
+
+def kv4_append(dims: Dims, cache: Kv4Cache, k_new, v_new, n_new: int, seq_lens=None, new_lens=None):
+    """Append up to n_new tokens a sequence, k_new / v_new [B, Hkv, n_new, D]; seq_lens count them already, up to dims.ctx_len."""
+    B, n = dims.batch, dims.batch * dims.n_kv_heads * n_new * dims.head_dim
+    st = _cache_stream(dims, cache)
+    rc = lib().a2ats_kv4_append(ctypes.byref(dims), cache.ref, _arg(cache, k_new, "k_new", cache.kv_dtype, n),
+                                _arg(cache, v_new, "v_new", cache.kv_dtype, n), n_new,
+                                _arg(cache, seq_lens, "seq_lens", torch.int32, B),
+                                _arg(cache, new_lens, "new_lens", torch.int32, B), st)
+    _check(rc, "a2ats_kv4_append")
+
+
+def kv4_read(dims: Dims, cache: Kv4Cache, n_rows: int, seq_lens, new_lens, k_out, v_out):
+    """The last tokens of each sequence (as an append with these lengths wrote them) as float32 or bfloat16, k_out / v_out
+    [B, Hkv, n_rows, D] of one type; either may be None."""
+    B, n = dims.batch, dims.batch * dims.n_kv_heads * n_rows * dims.head_dim
+    some = k_out if k_out is not None else v_out
+    if some is None:
+        raise ValueError("neither k_out nor v_out")
+    st = _cache_stream(dims, cache)
+    rc = lib().a2ats_kv4_read(ctypes.byref(dims), cache.ref, n_rows, _arg(cache, seq_lens, "seq_lens", torch.int32, B),
+                              _arg(cache, new_lens, "new_lens", torch.int32, B), _arg(cache, k_out, "k_out", some.dtype, n),
+                              _arg(cache, v_out, "v_out", some.dtype, n), _dtype_code(some), st)
+    _check(rc, "a2ats_kv4_read")
+
+
+def sparse_attn_kv4(dims: Dims, cache: Kv4Cache, q, q_rot, sel_idx, sel_count, n_sel: int, sel_size: int, shared: bool,
+                    window: int, n_sink: int, cos_win, sin_win, seq_lens, out, ws: Optional[torch.Tensor] = None):
+    """Attention over sinks, selection (tokens: sel_size 1, or blocks: sel_size cache.block) and window of a cache in 4 bits."""
+    n_q = dims.batch * dims.n_q_heads * dims.head_dim
+    n_h = dims.batch * (dims.n_kv_heads if shared else dims.n_q_heads)
+    n_w = max(window, 1) * (dims.head_dim // 2)
+    st = _cache_stream(dims, cache)
+    rc = lib().a2ats_sparse_attn_kv4(ctypes.byref(dims), cache.ref, _arg(cache, q, "q", cache.kv_dtype, n_q),
+                                     _arg(cache, q_rot, "q_rot", torch.float32, n_q),
+                                     _arg(cache, sel_idx, "sel_idx", torch.int32, n_h * n_sel),
+                                     _arg(cache, sel_count, "sel_count", torch.int32, n_h), n_sel, sel_size, int(shared), window,
+                                     n_sink, _arg(cache, cos_win, "cos_win", torch.float32, n_w),
+                                     _arg(cache, sin_win, "sin_win", torch.float32, n_w),
+                                     _arg(cache, seq_lens, "seq_lens", torch.int32, dims.batch),
+                                     _arg(cache, out, "out", cache.kv_dtype, n_q), _ws_ptr(cache, ws), _ws_bytes(ws), st)
+    _check(rc, "a2ats_sparse_attn_kv4")
+
+
+def _projected(dims: Dims, x: Optional[torch.Tensor], name: str, heads: int, n_new: int):
+    """Pointer and token stride of [B, n_new, heads * D] (or [B, n_new, heads, D]) whose tokens are one distance apart."""
+    if x is None:
+        return None, 0
+    D, shape = dims.head_dim, tuple(x.shape)
+    if shape not in ((dims.batch, n_new, heads * D), (dims.batch, n_new, heads, D)):
+        raise ValueError(f"{name} has shape {shape}, not {(dims.batch, n_new, heads * D)}")
+    s = x.stride()
+    # (the stride of an axis of length 1 says nothing)
+    if s[-1] != 1 or (x.dim() == 4 and heads > 1 and s[2] != D):
+        raise ValueError(f"{name}: the heads of a token lie behind each other")
+    stride = s[1] if n_new > 1 else (s[0] if dims.batch > 1 else heads * D)
+    if dims.batch > 1 and s[0] != n_new * stride:
+        raise ValueError(f"{name}: all tokens are the same distance apart")
+    return x.data_ptr(), stride
+
+
+def qk_norm_rope(dims: Dims, q, k, n_new: int, q_weight, k_weight, eps: float, cos_pos, sin_pos, seq_lens=None, new_lens=None,
+                 q_norm=None, k_norm=None, q_pos=None, k_pos=None):
+    """Norms of the heads of q [B, n_new, Hq * D] and k [B, n_new, Hkv * D] (slices of one projection, or tensors of their own; either
+    may be None), and their rotation by the tokens' positions (cos_pos, sin_pos [n_pos, D / 2], as rope_tables makes them for a
+    window of n_pos >= ctx_len).  Outputs [B, H, n_new, D]: *_norm not rotated, *_pos rotated; those that are None are not made."""
+    some = q if q is not None else k
+    if some is None:
+        raise ValueError("neither q nor k")
+    dev = some.get_device()
+    if dev < 0:
+        raise ValueError(f"the tensors are on {some.device}")
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {some.device}, the current device is {torch.cuda.current_device()}")
+    code = _dtype_code(some)
+    B, D, n_pos = dims.batch, dims.head_dim, 0
+    for name, x in (("q", q), ("k", k)):
+        if x is not None and (x.dtype != some.dtype or x.device != some.device):
+            raise TypeError(f"{name} is {x.dtype} on {x.device}, not {some.dtype} on {some.device}")
+    on = _Like(some.device, dev)
+    if cos_pos is not None:
+        n_pos = cos_pos.shape[0]
+    n_q, n_k = B * dims.n_q_heads * n_new * D, B * dims.n_kv_heads * n_new * D
+    qp, qs = _projected(dims, q, "q", dims.n_q_heads, n_new)
+    kp, ks = _projected(dims, k, "k", dims.n_kv_heads, n_new)
+    rc = lib().a2ats_qk_norm_rope(ctypes.byref(dims), qp, qs, kp, ks, code, n_new,
+                                  _arg(on, q_weight, "q_weight", torch.float32, D), _arg(on, k_weight, "k_weight", torch.float32, D),
+                                  eps, _arg(on, cos_pos, "cos_pos", torch.float32, n_pos * (D // 2)),
+                                  _arg(on, sin_pos, "sin_pos", torch.float32, n_pos * (D // 2)), n_pos,
+                                  _arg(on, seq_lens, "seq_lens", torch.int32, B), _arg(on, new_lens, "new_lens", torch.int32, B),
+                                  _arg(on, q_norm, "q_norm", some.dtype, n_q), _arg(on, k_norm, "k_norm", some.dtype, n_k),
+                                  _arg(on, q_pos, "q_pos", some.dtype, n_q), _arg(on, k_pos, "k_pos", some.dtype, n_k),
+                                  torch._C._cuda_getCurrentRawStream(dev))
+    _check(rc, "a2ats_qk_norm_rope")
+
+
+class _Like:
+    """A device that the tensors of a call are on."""
+
+    def __init__(self, device, index):
+        self.device, self.device_index = device, index
+
+
 def _ws_ptr(cache: KvBlocks, ws: Optional[torch.Tensor]):
     if ws is None:
         return None
@@ -610,30 +772,49 @@ class DecodeState:
 
 
 class BlockDecodeState:
-    """Device buffers for decode steps over a KvBlocks cache (allocation only; no arithmetic).  scores: whether a step leaves the
-    selected blocks' scores in block_score (which the attention does not need)."""
+    """Device buffers for decode steps over a KvBlocks cache or a Kv4Cache with bounds (allocation only; no arithmetic).  scores:
+    whether a step leaves the selected blocks' scores in block_score (which the attention does not need).  q_weight, k_weight, eps:
+    of a model that normalises the heads of its queries and keys; a step then takes them as they come from the projections."""
 
-    def __init__(self, dims: Dims, cache: KvBlocks, top_blocks: int, window: int, n_sink: int, inv_freq: torch.Tensor,
-                 wrope_b: int, shared: bool = False, scores: bool = True):
+    def __init__(self, dims: Dims, cache, top_blocks: int, window: int, n_sink: int, inv_freq: torch.Tensor,
+                 wrope_b: int, shared: bool = False, scores: bool = True, q_weight=None, k_weight=None, eps: float = 1e-6):
         self.dims, self.cache, self.top_blocks, self.window, self.n_sink, self.shared = dims, cache, top_blocks, window, n_sink, shared
-        B, Hq, D, dev = dims.batch, dims.n_q_heads, dims.head_dim, cache.device
-        heads = dims.n_kv_heads if shared else Hq
+        self.four_bits = isinstance(cache, Kv4Cache)
+        self.blocks = cache.blocks if self.four_bits else cache
+        if self.blocks is None or self.blocks.bounds is None:
+            raise ValueError("blocks are selected by bounds, which the cache does not have")
+        if (q_weight is None) != (k_weight is None):
+            raise ValueError("q_weight and k_weight are given together")
+        self.q_weight, self.k_weight, self.eps = q_weight, k_weight, eps
+        B, Hq, Hkv, D, dev = dims.batch, dims.n_q_heads, dims.n_kv_heads, dims.head_dim, cache.device
+        heads = Hkv if shared else Hq
         self.cos_b, self.sin_b, self.cos_win, self.sin_win = rope_tables(D, inv_freq, wrope_b, window, dev)
         self.q_rot = torch.empty(B, Hq, D, dtype=torch.float32, device=dev)
         self.block_idx = torch.empty(B, heads, top_blocks, dtype=torch.int32, device=dev)
         self.block_count = torch.empty(B, heads, dtype=torch.int32, device=dev)
         self.block_score = torch.empty(B, heads, top_blocks, dtype=torch.float32, device=dev) if scores else None
         self.out = torch.empty(B, Hq, D, dtype=cache.kv_dtype, device=dev)
-        n_ws = max(workspace_bytes(dims, OP_BLOCK_TOPK), workspace_bytes(dims, OP_ATTN_KV8, top_blocks * cache.block, window), 256)
+        if q_weight is not None:
+            self.q_norm = torch.empty(B, Hq, D, dtype=cache.kv_dtype, device=dev)
+            self.k_norm = torch.empty(B, Hkv, 1, D, dtype=cache.kv_dtype, device=dev)
+        n_ws = max(workspace_bytes(dims, OP_BLOCK_TOPK),
+                   workspace_bytes(dims, OP_ATTN_KV4 if self.four_bits else OP_ATTN_KV8, top_blocks * cache.block, window), 256)
         self.ws = torch.empty(n_ws, dtype=torch.uint8, device=dev)
 
     def step(self, q, k_new, v_new, seq_lens=None):
-        """kv8_append of one token a sequence -> block_topk -> sparse_attn_kv8 on the current stream; returns self.out.
+        """qk_norm_rope (if there are weights) -> append of one token a sequence -> block_topk -> attention on the current stream;
+        returns self.out.  q [B, Hq, D], k_new, v_new [B, Hkv, 1, D].
         seq_lens counts that token already and is at most dims.ctx_len (None: ctx_len): a cache is made with room for what it
         is to hold, a larger length is taken as ctx_len and the token replaces the last one."""
-        kv8_append(self.dims, self.cache, k_new, v_new, 1, seq_lens)
-        block_topk(self.dims, self.cache, q, self.cos_b, self.sin_b, self.q_rot, self.shared, self.top_blocks, self.window,
+        dims = self.dims
+        append, attend = (kv4_append, sparse_attn_kv4) if self.four_bits else (kv8_append, sparse_attn_kv8)
+        if self.q_weight is not None:
+            qk_norm_rope(dims, q.reshape(dims.batch, 1, -1), k_new.reshape(dims.batch, 1, -1), 1, self.q_weight, self.k_weight, self.eps,
+                         None, None, seq_lens, None, q_norm=self.q_norm, k_norm=self.k_norm)
+            q, k_new = self.q_norm, self.k_norm
+        append(dims, self.cache, k_new, v_new, 1, seq_lens)
+        block_topk(dims, self.blocks, q, self.cos_b, self.sin_b, self.q_rot, self.shared, self.top_blocks, self.window,
                    self.n_sink, seq_lens, self.block_idx, self.block_count, self.block_score, ws=self.ws)
-        sparse_attn_kv8(self.dims, self.cache, q, self.q_rot, self.block_idx, self.block_count, self.top_blocks, self.cache.block,
-                        self.shared, self.window, self.n_sink, self.cos_win, self.sin_win, seq_lens, self.out, self.ws)
+        attend(dims, self.cache, q, self.q_rot, self.block_idx, self.block_count, self.top_blocks, self.cache.block,
+               self.shared, self.window, self.n_sink, self.cos_win, self.sin_win, seq_lens, self.out, self.ws)
         return self.out

@@ -92,6 +92,24 @@ int check_blocks(const a2ats_dims& d, const a2ats_kv_blocks* c, bool rows, bool 
   return A2ATS_OK;
 }
 
+// The same of a cache in 4 bits.
+int check_kv4(const a2ats_dims& d, const a2ats_kv4* c, a2ats::Kv4Cache* m) {
+  if (!c) return A2ATS_ERR_INVALID_ARG;
+  a2ats_kv_blocks blocks = {};
+  blocks.bounds = c->bounds;
+  blocks.page_table = c->page_table;
+  blocks.page_size = c->page_size;
+  blocks.block = c->block;
+  blocks.kv_dtype = c->kv_dtype;
+  *m = {};
+  const int rc = check_blocks(d, &blocks, false, false, &m->at);
+  if (rc != A2ATS_OK) return rc;
+  if (!c->rows || misaligned16(c->rows) || !c->scales || ((uintptr_t)c->scales & 7u)) return A2ATS_ERR_INVALID_ARG;
+  m->rows = (uint8_t*)c->rows;
+  m->scales = (uint8_t*)c->scales;
+  return A2ATS_OK;
+}
+
 // Whether `ws` can hold a selection plan's workspace.  The streaming route refuses to run without; a
 // wide plan then takes the exact route instead, which needs none (selections of more than 2048 tokens
 // used to ask for no workspace at all).
@@ -166,6 +184,12 @@ size_t a2ats_workspace_bytes(const a2ats_dims* d, int op, int32_t top_k, int32_t
       if (top_k < 0 || window < 0) return (size_t)-1;
       const size_t own = a2ats::make_kv8_plan(*d, top_k, window, false).bytes;
       const size_t shared = a2ats::make_kv8_plan(*d, top_k, window, true).bytes;
+      return own > shared ? own : shared;
+    }
+    case A2ATS_OP_ATTN_KV4: {
+      if (top_k < 0 || window < 0) return (size_t)-1;
+      const size_t own = a2ats::make_kv4_plan(*d, top_k, window, false).bytes;
+      const size_t shared = a2ats::make_kv4_plan(*d, top_k, window, true).bytes;
       return own > shared ? own : shared;
     }
     case A2ATS_OP_FIT: return a2ats::fit_ws_bytes(*d);
@@ -758,6 +782,86 @@ int a2ats_sparse_attn_kv8(const a2ats_dims* d, const a2ats_kv_blocks* blocks, co
   const hipError_t e = a2ats::launch_sparse_attn_kv8(*d, m, blocks->kv_dtype, blocks->format, q, q_rot, sel_idx, sel_count, n_sel,
                                                      log2_of(sel_size), shared != 0, window, n_sink, cos_win, sin_win, seq_lens,
                                                      out, ws, (hipStream_t)stream);
+  return e == hipSuccess ? A2ATS_OK : A2ATS_ERR_HIP;
+}
+
+int a2ats_kv4_append(const a2ats_dims* d, const a2ats_kv4* cache, const void* k_new, const void* v_new, int32_t n_new,
+                     const int32_t* seq_lens, const int32_t* new_lens, void* stream) {
+  int rc = check_dims(d);
+  if (rc != A2ATS_OK) return rc;
+  a2ats::Kv4Cache m;
+  rc = check_kv4(*d, cache, &m);
+  if (rc != A2ATS_OK) return rc;
+  if (n_new < 0 || n_new > d->ctx_len) return A2ATS_ERR_INVALID_ARG;
+  if (n_new == 0) return A2ATS_OK;
+  if (!launchable(*d, d->n_kv_heads, 2 * (int64_t)a2ats::append_parts(n_new, cache->block), a2ats::append_threads(cache->block)))
+    return A2ATS_ERR_UNSUPPORTED;
+  if (!k_new || !v_new || misaligned16(k_new) || misaligned16(v_new)) return A2ATS_ERR_INVALID_ARG;
+  const hipError_t e = a2ats::launch_kv4_append(*d, m, cache->kv_dtype, k_new, v_new, n_new, seq_lens, new_lens, (hipStream_t)stream);
+  return e == hipSuccess ? A2ATS_OK : A2ATS_ERR_HIP;
+}
+
+int a2ats_kv4_read(const a2ats_dims* d, const a2ats_kv4* cache, int32_t n_rows, const int32_t* seq_lens, const int32_t* new_lens,
+                   void* k_out, void* v_out, int out_dtype, void* stream) {
+  int rc = check_dims(d);
+  if (rc != A2ATS_OK) return rc;
+  a2ats::Kv4Cache m;
+  rc = check_kv4(*d, cache, &m);
+  if (rc != A2ATS_OK) return rc;
+  if (n_rows < 0 || n_rows > d->ctx_len || (out_dtype != A2ATS_F32 && out_dtype != A2ATS_BF16)) return A2ATS_ERR_INVALID_ARG;
+  if (n_rows == 0) return A2ATS_OK;
+  if (!launchable(*d, d->n_kv_heads, ((int64_t)n_rows + a2ats::kKv4ReadRows - 1) / a2ats::kKv4ReadRows, 256))
+    return A2ATS_ERR_UNSUPPORTED;
+  if ((!k_out && !v_out) || misaligned16(k_out) || misaligned16(v_out)) return A2ATS_ERR_INVALID_ARG;
+  const hipError_t e = a2ats::launch_kv4_read(*d, m, n_rows, seq_lens, new_lens, k_out, v_out, out_dtype, (hipStream_t)stream);
+  return e == hipSuccess ? A2ATS_OK : A2ATS_ERR_HIP;
+}
+
+int a2ats_sparse_attn_kv4(const a2ats_dims* d, const a2ats_kv4* cache, const void* q, const float* q_rot, const int32_t* sel_idx,
+                          const int32_t* sel_count, int32_t n_sel, int32_t sel_size, int32_t shared, int32_t window, int32_t n_sink,
+                          const float* cos_win, const float* sin_win, const int32_t* seq_lens, void* out, void* ws, size_t ws_bytes,
+                          void* stream) {
+  int rc = check_dims(d);
+  if (rc != A2ATS_OK) return rc;
+  a2ats::Kv4Cache m;
+  rc = check_kv4(*d, cache, &m);
+  if (rc != A2ATS_OK) return rc;
+  if (n_sel < 0 || window < 0 || n_sink < 0) return A2ATS_ERR_INVALID_ARG;
+  if (sel_size != 1 && sel_size != cache->block) return A2ATS_ERR_INVALID_ARG;
+  if (n_sel > 4096) return A2ATS_ERR_UNSUPPORTED;
+  const a2ats::Kv4Plan plan = a2ats::make_kv4_plan(*d, (long)n_sel * sel_size, window, shared != 0);
+  if (!launchable(*d, d->n_q_heads, plan.parts, 256)) return A2ATS_ERR_UNSUPPORTED;
+  if (plan.bytes > 0 && (!ws || misaligned16(ws) || ws_bytes < plan.bytes)) return A2ATS_ERR_WORKSPACE;
+  if (!q || !q_rot || !sel_count || !out || (n_sel > 0 && !sel_idx)) return A2ATS_ERR_INVALID_ARG;
+  if (window > 0 && (!cos_win || !sin_win)) return A2ATS_ERR_INVALID_ARG;
+  if (misaligned16(q) || misaligned16(q_rot) || misaligned16(cos_win) || misaligned16(sin_win)) return A2ATS_ERR_INVALID_ARG;
+  const hipError_t e = a2ats::launch_sparse_attn_kv4(*d, m, cache->kv_dtype, q, q_rot, sel_idx, sel_count, n_sel, log2_of(sel_size),
+                                                     shared != 0, window, n_sink, cos_win, sin_win, seq_lens, out, ws,
+                                                     (hipStream_t)stream);
+  return e == hipSuccess ? A2ATS_OK : A2ATS_ERR_HIP;
+}
+
+int a2ats_qk_norm_rope(const a2ats_dims* d, const void* q, int64_t q_stride, const void* k, int64_t k_stride, int dtype, int32_t n_new,
+                       const float* q_weight, const float* k_weight, float eps, const float* cos_pos, const float* sin_pos,
+                       int32_t n_pos, const int32_t* seq_lens, const int32_t* new_lens, void* q_norm, void* k_norm, void* q_pos,
+                       void* k_pos, void* stream) {
+  const int rc = check_dims(d);
+  if (rc != A2ATS_OK) return rc;
+  if (dtype != A2ATS_F32 && dtype != A2ATS_BF16) return A2ATS_ERR_INVALID_ARG;
+  if (n_new < 0 || n_new > d->ctx_len || !(eps >= 0x1p-126f && eps <= 1.f)) return A2ATS_ERR_INVALID_ARG;
+  if (n_new == 0) return A2ATS_OK;
+  if (!q && !k) return A2ATS_ERR_INVALID_ARG;
+  if (q ? q_stride < (int64_t)d->n_q_heads * d->head_dim || q_stride % 8 : q_norm || q_pos) return A2ATS_ERR_INVALID_ARG;
+  if (k ? k_stride < (int64_t)d->n_kv_heads * d->head_dim || k_stride % 8 : k_norm || k_pos) return A2ATS_ERR_INVALID_ARG;
+  if ((q && !q_norm && !q_pos) || (k && !k_norm && !k_pos)) return A2ATS_ERR_INVALID_ARG;
+  if ((q_pos || k_pos) && (!cos_pos || !sin_pos || n_pos < d->ctx_len)) return A2ATS_ERR_INVALID_ARG;
+  for (const void* p : {q, k, (const void*)q_weight, (const void*)k_weight, (const void*)cos_pos, (const void*)sin_pos,
+                        (const void*)q_norm, (const void*)k_norm, (const void*)q_pos, (const void*)k_pos})
+    if (misaligned16(p)) return A2ATS_ERR_INVALID_ARG;
+  if ((double)a2ats::qk_norm_waves(*d, n_new, q != nullptr, k != nullptr) * 64.0 >= 4294967296.0 - 256.0) return A2ATS_ERR_UNSUPPORTED;
+  const a2ats::QkNormArgs a = {q, k, q_stride, k_stride, q_weight, k_weight, eps, cos_pos, sin_pos, seq_lens, new_lens,
+                               q_norm, k_norm, q_pos, k_pos};
+  const hipError_t e = a2ats::launch_qk_norm_rope(*d, dtype, n_new, a, (hipStream_t)stream);
   return e == hipSuccess ? A2ATS_OK : A2ATS_ERR_HIP;
 }
 

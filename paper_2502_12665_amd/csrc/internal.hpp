@@ -10,6 +10,7 @@
 
 #include "a2ats.h"
 #include "common.hpp"
+#include "kv4.hpp"
 #include "kv_blocks.hpp"
 
 namespace a2ats {
@@ -217,6 +218,35 @@ hipError_t launch_sparse_attn_kv8(const a2ats_dims& d, const BlockCache& m, int 
                                   const float* q_rot, const int32_t* sel_idx, const int32_t* sel_count, int n_sel, int sel_shift,
                                   bool shared, int window, int n_sink, const float* cos_win, const float* sin_win,
                                   const int32_t* seq_lens, void* out, void* ws, hipStream_t stream);
+// Joins the states of `heads` heads' parts (at most 32): [128 sums, maximum, sum of weights] each.
+hipError_t launch_attn_merge(int kv_dtype, const float* partial, void* out, int heads, int parts, hipStream_t stream);
+
+// A cache in 4 bits (kv4.hpp): append, read back, attention; norms and rotation of queries and keys.
+hipError_t launch_kv4_append(const a2ats_dims& d, const Kv4Cache& m, int kv_dtype, const void* k_new, const void* v_new, int n_new,
+                             const int32_t* seq_lens, const int32_t* new_lens, hipStream_t stream);
+constexpr int kKv4ReadRows = 64;   // rows of a workgroup of 256 threads
+hipError_t launch_kv4_read(const a2ats_dims& d, const Kv4Cache& m, int n_rows, const int32_t* seq_lens, const int32_t* new_lens,
+                           void* k_out, void* v_out, int out_dtype, hipStream_t stream);
+struct Kv4Plan {
+  int parts;            // as Kv8Plan
+  size_t bytes;
+};
+Kv4Plan make_kv4_plan(const a2ats_dims& d, long sel_rows, int window, bool shared);
+hipError_t launch_sparse_attn_kv4(const a2ats_dims& d, const Kv4Cache& m, int kv_dtype, const void* q, const float* q_rot,
+                                  const int32_t* sel_idx, const int32_t* sel_count, int n_sel, int sel_shift, bool shared, int window,
+                                  int n_sink, const float* cos_win, const float* sin_win, const int32_t* seq_lens, void* out,
+                                  void* ws, hipStream_t stream);
+struct QkNormArgs {
+  const void *q, *k;
+  int64_t q_stride, k_stride;          // elements from one token to the next
+  const float *q_weight, *k_weight;    // nullptr: ones
+  float eps;
+  const float *cos_pos, *sin_pos;
+  const int32_t *seq_lens, *new_lens;
+  void *q_norm, *k_norm, *q_pos, *k_pos;
+};
+long qk_norm_waves(const a2ats_dims& d, int n_new, bool q, bool k);   // of 64 threads, in all
+hipError_t launch_qk_norm_rope(const a2ats_dims& d, int dtype, int n_new, const QkNormArgs& a, hipStream_t stream);
 
 // Copy freshly encoded code rows [B][Hkv][n_new][row_bytes] to tokens pos0 .. pos0 + n_new - 1 of a paged pool.
 hipError_t launch_codes_to_pages(const a2ats_dims& d, const uint8_t* rows, int n_new, int pos0, int row_bytes,

@@ -19,17 +19,13 @@
 // the requests that wait for each other (length, rows, bounds).  Requesting the bounds and the tail's rows ahead of the barrier did
 // not shorten it (4.9).
 #include "internal.hpp"
-#include "kv_blocks.hpp"
+#include "kv_bounds.hpp"
 
 namespace a2ats {
 namespace {
 
-constexpr int kWaveRows = 16;                                     // rows that a wave holds
 constexpr uint32_t kTinyBits = (127u - 100u) << 23;               // 2^-100
 constexpr uint32_t kInfBits = 0x7f800000u;
-
-// Four or eight waves: a slab of 64 rows, or the largest block.
-constexpr int append_waves(int block) { return block > 64 ? 8 : 4; }
 
 // rint(127 x / a), ties to even, decided as for real numbers: within a half of k the two sides of  254 |x| <> (2 k + 1) a  are
 // formed exactly in float64 (32 bits each).
@@ -42,37 +38,6 @@ __device__ __forceinline__ int code_i8_close(float x, float a) {
     c = (int)k + (lhs > rhs ? 1 : (lhs < rhs ? 0 : ((int)k & 1)));
   }
   return x < 0.f ? -c : c;
-}
-
-// min / max that keep a NaN once there is one.
-__device__ __forceinline__ float low(float a, float b) { return (b < a || b != b) ? b : a; }
-__device__ __forceinline__ float high(float a, float b) { return (b > a || b != b) ? b : a; }
-
-__device__ __forceinline__ void put_elem(float* p, float v) { *p = v; }
-__device__ __forceinline__ void put_elem(uint16_t* p, float v) { *p = (uint16_t)(__float_as_uint(v) >> 16); }   // (v was a bfloat16)
-__device__ __forceinline__ float get_elem(const float* p) { return *p; }
-__device__ __forceinline__ float get_elem(const uint16_t* p) { return bf16_to_f32(*p); }
-
-// Plain min / max (fminf would first quiet both operands).
-__device__ __forceinline__ float min2(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, -INFINITY); }
-__device__ __forceinline__ float max2(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, INFINITY); }
-
-// f over the four lane rows of eight values v[e]: lane row r is left with two of them, 4 (r / 2) + 2 (r % 2) + {0, 1}.
-template <typename F>
-__device__ __forceinline__ float2 over_lane_rows(const float (&v)[8], F f) {
-  float h[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[e]), __float_as_uint(v[e + 4]), false, false);
-    h[e] = f(__uint_as_float(s[0]), __uint_as_float(s[1]));
-  }
-  float q[2];
-#pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(h[e]), __float_as_uint(h[e + 2]), false, false);
-    q[e] = f(__uint_as_float(s[0]), __uint_as_float(s[1]));
-  }
-  return make_float2(q[0], q[1]);
 }
 
 // CODES: the 8-bit cache is written (else only the bounds are).  E4M3: its format.  NW: waves of a workgroup.

@@ -1,0 +1,141 @@
+// Norms of queries and keys, head by head, and their rotation by the tokens' positions, in one pass:
+//     y = x w / sqrt(mean(x^2) + eps),   y R_p,
+// each output rounded once, from float32.  Sums of squares are those of x 2^-e, |x| < 2 * 2^e, so that no square overflows; e >= -60,
+// so that eps 2^-2e does not either.
+//
+// A stream: 128 e bytes a head in, as many for each output.  16 lanes a row, a wave four rows at a time of one token, so that
+// the token's angles are loaded once for 16 heads; the other half of a rotated pair is eight lanes on.
+#include "internal.hpp"
+#include "kv_blocks.hpp"
+
+namespace a2ats {
+namespace {
+
+constexpr int D = 128;
+constexpr int kWaveHeads = 16;
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t lane_of(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false);
+}
+template <int CTRL>
+__device__ __forceinline__ float lane_of(float v) { return __uint_as_float(lane_of<CTRL>(__float_as_uint(v))); }
+
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+  *(float4*)p = make_float4(x[0], x[1], x[2], x[3]);
+  *(float4*)(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+}
+__device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8]) {
+  typedef __attribute__((ext_vector_type(2))) float f32x2;
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){x[2 * i], x[2 * i + 1]}, bf16x2));   // (to the nearest)
+  *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Waves: [b][token][chunk of 16 heads]; the queries' heads before the keys'.
+template <typename T>
+__global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkNormArgs a, int batch, int Hq, int Hkv, int n_new, int ctx_len, int chunks) {
+  const uint32_t wave = blockIdx.x * 4 + (threadIdx.x >> 6), token = wave / (uint32_t)chunks;   // (fewer than 2^26)
+  const int chunk = (int)(wave % (uint32_t)chunks), b = (int)(token / (uint32_t)n_new), t = (int)(token % (uint32_t)n_new);
+  if (b >= batch) return;
+  int n = a.seq_lens ? a.seq_lens[b] : ctx_len;
+  n = min(max(n, 0), ctx_len);
+  int cnt = a.new_lens ? a.new_lens[b] : n_new;
+  cnt = min(max(cnt, 0), min(n_new, n));
+  if (t >= cnt) return;
+  const int lane = threadIdx.x & 63, slot = lane >> 4, j = lane & 15;
+  const int first = a.q ? 0 : Hq, last = a.k ? Hq + Hkv : Hq;
+  const int h0 = first + chunk * kWaveHeads;
+
+  float x[4][8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int h = h0 + i * 4 + slot;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
+    if (h < last) {
+      const T* from = h < Hq ? (const T*)a.q + (size_t)token * a.q_stride + (size_t)h * D
+                             : (const T*)a.k + (size_t)token * a.k_stride + (size_t)(h - Hq) * D;
+      load8(from + j * 8, x[i]);
+    }
+  }
+  const bool turn = a.q_pos != nullptr || a.k_pos != nullptr;
+  float cs[8], sn[8];
+  if (turn) {
+    const size_t at = (size_t)(n - cnt + t) * (D / 2) + (j & 7) * 8;
+    load8(a.cos_pos + at, cs);
+    load8(a.sin_pos + at, sn);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sn[e] = j < 8 ? -sn[e] : sn[e];
+  }
+  float wq[8], wk[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) wq[e] = wk[e] = 1.f;
+  if (a.q_weight) load8(a.q_weight + j * 8, wq);
+  if (a.k_weight) load8(a.k_weight + j * 8, wk);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int h = h0 + i * 4 + slot;
+    uint32_t big = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) big = max(big, __float_as_uint(x[i][e]) & 0x7fffffffu);
+    big = max(big, lane_of<0xB1>(big));    // quad_perm [1,0,3,2]
+    big = max(big, lane_of<0x4E>(big));    // quad_perm [2,3,0,1]
+    big = max(big, lane_of<0x124>(big));   // row_ror:4
+    big = max(big, lane_of<0x128>(big));   // row_ror:8
+    const int e0 = min(max((int)(big >> 23) - 127, -60), 126);
+    const float down = __uint_as_float((uint32_t)(127 - e0) << 23);
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x[i][e] *= down;
+      sum += x[i][e] * x[i][e];
+    }
+    sum += lane_of<0xB1>(sum);
+    sum += lane_of<0x4E>(sum);
+    sum += lane_of<0x124>(sum);
+    sum += lane_of<0x128>(sum);
+    const float r = rsqrtf(sum * (1.f / D) + ldexpf(a.eps, -2 * e0));
+    const bool query = h < Hq;
+    float y[8], z[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = x[i][e] * r * (query ? wq[e] : wk[e]);
+    if (turn) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] = y[e] * cs[e] + lane_of<0x128>(y[e]) * sn[e];
+    }
+    if (h < last) {
+      const size_t to = (query ? (((size_t)b * Hq + h) * n_new + t) : (((size_t)b * Hkv + h - Hq) * n_new + t)) * D + j * 8;
+      T* norm = (T*)(query ? a.q_norm : a.k_norm);
+      T* pos = (T*)(query ? a.q_pos : a.k_pos);
+      if (norm) store8(norm + to, y);
+      if (pos) store8(pos + to, z);
+    }
+  }
+}
+
+}  // namespace
+
+static int norm_chunks(const a2ats_dims& d, bool q, bool k) {
+  return ((q ? d.n_q_heads : 0) + (k ? d.n_kv_heads : 0) + kWaveHeads - 1) / kWaveHeads;
+}
+long qk_norm_waves(const a2ats_dims& d, int n_new, bool q, bool k) { return (long)d.batch * n_new * norm_chunks(d, q, k); }
+
+hipError_t launch_qk_norm_rope(const a2ats_dims& d, int dtype, int n_new, const QkNormArgs& a, hipStream_t stream) {
+  const long waves = qk_norm_waves(d, n_new, a.q != nullptr, a.k != nullptr);
+  if (waves == 0 || d.ctx_len == 0) return hipSuccess;
+  const int chunks = norm_chunks(d, a.q != nullptr, a.k != nullptr);
+  const dim3 grid((unsigned)((waves + 3) / 4));
+  if (dtype == A2ATS_BF16)
+    hipLaunchKernelGGL((qk_norm_rope_kernel<uint16_t>), grid, dim3(256), 0, stream, a, d.batch, d.n_q_heads, d.n_kv_heads, n_new,
+                       d.ctx_len, chunks);
+  else
+    hipLaunchKernelGGL((qk_norm_rope_kernel<float>), grid, dim3(256), 0, stream, a, d.batch, d.n_q_heads, d.n_kv_heads, n_new,
+                       d.ctx_len, chunks);
+  return hipGetLastError();
+}
+
+}  // namespace a2ats
