@@ -45,236 +45,185 @@ struct Attn4Args {
   int32_t parts, far_share, win_share;   // workgroups of a head's (KV head's) rows, and how many of them each takes
 };
 
-// The rows of a pair of tiles as they come from memory: 32 dimensions of the key of row `column` of either tile; of the values of
-// the rows 4 * lane row + 0 .. 3 of either, two dimensions of each group.
-struct PairRows {
-  uint4 k[2];
-  uint32_t v[8];
-};
-// Where the rows of two pairs are in the cache, the keys' scale bytes, what the finished product is multiplied by, 0 or, for a
-// place without a row, all bits, and the values' scales by group: of a wave, in LDS.
-struct alignas(16) PairPlaces {
-  uint32_t row[2 * kPair];
-  uint32_t ksc[2 * kPair];
-  float ks[2 * kPair];
-  uint32_t none[2 * kPair];
-  float vs[4][2 * kPair];
-};
+constexpr int kUnit = 64;   // rows that a wave takes at a time: four tiles of 16, a row for each lane
 
-// A wave's running softmax: a head in each column (the same m in all lane rows, l of the lane's own rows), and its output,
-// o[t][i] being dimension 32 (t / 2) + 2 (4 * lane row + i) + t % 2, in the columns of group t / 2.
-struct WaveState {
-  float m, l;
-  f32x4 o[8];
-};
-
+// Heads that attend the same rows, padded to NH: what rows and columns of the tiles stand for.
+//   first product: row m of the queries is (head, term); its results are rows 4 * lane row + i, so that the terms of a head are in one lane:
+//     NH 1: term m % 4, in each lane row alike; 4: head m / 4, term m % 4; 8: head m / 2, term m % 2 (the third one is a product of its own)
+//   second product: column c of the weights is
+//     NH 1: term c / 4 and group c % 4; 4: head c / 4 and group c % 4; 8: head c / 2 and half c % 2 of the groups, of which there are two sets
 template <int NH>
-struct Columns {
-  static constexpr int kTerms = NH == 8 ? 2 : 4;   // of the query: columns of a head in the first product
-  // Which head, term of the query, group (eight heads: half of the groups) and term of the weights a column has.
-  static __device__ __forceinline__ int head(int col) { return NH == 1 ? 0 : col % NH; }
-  static __device__ __forceinline__ int q_term(int col) { return NH == 1 ? col & 3 : col / NH; }
-  static __device__ __forceinline__ int group(int col) { return NH == 1 ? col & 3 : col / NH; }
-  static __device__ __forceinline__ int w_term(int col) { return NH == 1 ? col >> 2 : 0; }
-  // The sum over the terms of the query: the same bits in each column of a head.
-  static __device__ __forceinline__ float sum(float v) {
-    if (NH == 1) {
-      v += dpp<0xB1>(v);   // quad_perm [1,0,3,2]
-      v += dpp<0x4E>(v);   // quad_perm [2,3,0,1]
-      return v;
-    }
-    return head_sum<NH == 1 ? 4 : NH>(v);
-  }
+struct Layout {
+  static constexpr int kOwn = NH == 1 ? 1 : (NH == 4 ? 4 : 8);   // logits of a lane in a unit
+  static constexpr int kHeads = NH == 8 ? 2 : 1;                 // heads that a lane has logits of
+  static constexpr int kColumns = NH == 1 ? 13 : 48;             // of weights in LDS (one head: 12 and one of zeros; else 3 terms of 16)
+  static __device__ __forceinline__ int q_head(int m) { return NH == 1 ? 0 : m * NH / 16; }
+  static __device__ __forceinline__ int q_term(int m) { return NH == 8 ? m & 1 : m & 3; }
+  static __device__ __forceinline__ int col_head(int c) { return NH == 1 ? 0 : c * NH / 16; }
 };
 
-__device__ __forceinline__ void load_pair(const uint8_t* cache, const uint32_t* rows, int col, int lrow, PairRows& p) {
-#pragma unroll
-  for (int t = 0; t < 2; ++t) p.k[t] = *(const uint4*)(cache + (size_t)rows[t * 16 + col] * kKv4RowBytes + lrow * 16);
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const uint4 r4 = *(const uint4*)(rows + t * 16 + lrow * 4);
-    const uint32_t r[4] = {r4.x, r4.y, r4.z, r4.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) p.v[4 * t + i] = *(const uint32_t*)(cache + (size_t)r[i] * kKv4RowBytes + kKv4Half + col * 4);
-  }
-}
-// The keys of window rows: elements 16 * lane row + 0 .. 15 of either half.
-__device__ __forceinline__ void load_turned_pair(const uint8_t* cache, const uint32_t* rows, int col, int lrow, PairRows& p) {
-  load_pair(cache, rows, col, lrow, p);
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const uint8_t* from = cache + (size_t)rows[t * 16 + col] * kKv4RowBytes + lrow * 8;
-    const uint2 a = *(const uint2*)from, b = *(const uint2*)(from + 32);
-    p.k[t] = make_uint4(a.x, a.y, b.x, b.y);
-  }
-}
+// A wave's working memory in LDS.
+template <int NH>
+struct alignas(16) WaveMemory {
+  uint16_t weights[Layout<NH>::kColumns][kUnit];   // bfloat16
+  i32x4 values[kUnit][4];                          // a unit's values as they come from memory
+  uint32_t row[2][kUnit];                          // where a unit's rows are, and the next one's
+  uint32_t ksc[kUnit];                             // scale bytes of the keys
+  uint32_t vsc[NH == 1 ? 1 : kUnit];               // ... of the values (one head: a lane has its own row's)
+  float ks[NH == 1 ? 1 : kUnit];                   // 1, or NaN for a key that is; -1 without a row
+  float win_ks[kUnit];                             // window rows: the largest of the key's scales
+  float alpha[8];
+};
 
-// The weights of the two tiles' rows of a lane, from their products with the queries (times log2 e / sqrt(128)); the state's
-// maximum and sum.
-__device__ __forceinline__ void pair_weights(const f32x4 (&dot)[2], const PairPlaces& pl, int first, int lrow, WaveState& st,
-                                             float (&w)[8]) {
-  float lg[8];
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const int at = first + t * 16 + lrow * 4;
-    const float4 k4 = *(const float4*)(pl.ks + at);
-    const uint4 n4 = *(const uint4*)(pl.none + at);
-    const float kk[4] = {k4.x, k4.y, k4.z, k4.w};
-    const uint32_t nn[4] = {n4.x, n4.y, n4.z, n4.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      lg[4 * t + i] = __uint_as_float((nn[i] & 0xff800000u) | (~nn[i] & __float_as_uint(dot[t][i] * kk[i])));   // (-inf)
-  }
-  float mx = lg[0];
-#pragma unroll
-  for (int i = 1; i < 8; ++i) mx = fmaxf(mx, lg[i]);
-  const float mn = fmaxf(st.m, rows_max(mx));
-  if (__builtin_amdgcn_ballot_w64(mn > st.m)) {
-    const float alpha = power(st.m - mn);
-    st.l *= alpha;
-#pragma unroll
-    for (int t = 0; t < 8; ++t) st.o[t] *= alpha;
-    st.m = mn;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    w[i] = power(lg[i] - mn);
-    st.l += w[i];
-  }
-}
+// The queries as the first operand, of a workgroup: made once, and read again for each unit (16 registers that four waves a SIMD do
+// not have).
+template <int NH>
+struct alignas(16) Queries {
+  uint4 far[4][64], win[4][64];
+  uint4 third[NH == 8 ? 4 : 1][64];
+  float win_scale[64];
+};
+
+// The upper half of a float: bfloat16 by truncation, and what is left.
+__device__ __forceinline__ float lower_part(float x) { return x - __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+__device__ __forceinline__ uint16_t upper_half(float x) { return (uint16_t)(__float_as_uint(x) >> 16); }
 
 __device__ __forceinline__ bf16x8 pack8(const float (&x)[8]) {
   return __builtin_bit_cast(bf16x8, make_uint4(upper_halves(x[0], x[1]), upper_halves(x[2], x[3]), upper_halves(x[4], x[5]),
                                                upper_halves(x[6], x[7])));
 }
-// What is left of x without its upper half.
-__device__ __forceinline__ float lower_part(float x) { return x - __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
 
-// The pair's values times its weights.
+// Slice i of the far queries: elements 32 * lane row + 8 i + 0 .. 7 of the head of the lane's row, as bfloat16 terms by truncation.
 template <int NH>
-__device__ __forceinline__ void absorb_values(const float (&weight)[8], const PairPlaces& pl, int first, int col, int lrow,
-                                              const PairRows& p, WaveState& st) {
-  // Weights times the scales of the column's group, as bfloat16 terms.
-  constexpr int kSets = NH == 8 ? 2 : 1, kTerms = NH == 1 ? 1 : 3;
-  bf16x8 b[kSets][kTerms];
+__device__ __forceinline__ void put_far_queries(const float* from, int i, bool active, int lane, Queries<NH>& to) {
+  const int term = Layout<NH>::q_term(lane & 15);
+  const uint32_t cut1 = term >= 1 ? 0xffff0000u : 0u, cut2 = term >= 2 ? 0xffff0000u : 0u, keep = active && term < 3 ? ~0u : 0u;
+  float y[8], z[8];
+  load8(from + 8 * i, y);
 #pragma unroll
-  for (int set = 0; set < kSets; ++set) {
-    const int g = NH == 8 ? 2 * Columns<NH>::group(col) + set : Columns<NH>::group(col);
-    float x[8];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const float4 s4 = *(const float4*)(pl.vs[g] + first + t * 16 + lrow * 4);
-      const float ss[4] = {s4.x, s4.y, s4.z, s4.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[4 * t + i] = weight[4 * t + i] * ss[i];
-    }
-    if constexpr (NH == 1) {
-      const int term = Columns<NH>::w_term(col);
-      const uint32_t cut1 = term >= 1 ? 0xffff0000u : 0u, cut2 = term >= 2 ? 0xffff0000u : 0u, cut3 = term >= 3 ? 0u : ~0u;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        x[i] -= __uint_as_float(__float_as_uint(x[i]) & cut1);
-        x[i] -= __uint_as_float(__float_as_uint(x[i]) & cut2);
-        x[i] = __uint_as_float(__float_as_uint(x[i]) & cut3);
-      }
-      b[0][0] = pack8(x);
-    } else {
-#pragma unroll
-      for (int term = 0; term < kTerms; ++term) {
-        b[set][term] = pack8(x);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = lower_part(x[i]);
-      }
-    }
+  for (int e = 0; e < 8; ++e) {
+    y[e] *= kLogit;
+    z[e] = __uint_as_float(__float_as_uint(lower_part(lower_part(y[e]))) & (term == 0 ? keep : 0u));
+    y[e] -= __uint_as_float(__float_as_uint(y[e]) & cut1);
+    if (NH != 8) y[e] -= __uint_as_float(__float_as_uint(y[e]) & cut2);
+    y[e] = __uint_as_float(__float_as_uint(y[e]) & keep);
   }
-  // Rows 2 i and 2 i + 1: byte g of even[i] has the first of the two dimensions of group g, of odd[i] the second; the lower half
-  // of a byte is the first row's.
-  uint32_t even[4], odd[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t a = p.v[2 * i], c = p.v[2 * i + 1];
-    even[i] = (a & 0x0f0f0f0fu) | ((c << 4) & 0xf0f0f0f0u);
-    odd[i] = ((a >> 4) & 0x0f0f0f0fu) | (c & 0xf0f0f0f0u);
-  }
-#define A2ATS_TILE(t)                                                                                                           \
-  {                                                                                                                             \
-    uint32_t w[4];                                                                                                              \
-    _Pragma("unroll") for (int i = 0; i < 4; ++i)                                                                               \
-        w[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((t) & 1 ? odd[i] : even[i], 1.f, (t) / 2)); \
-    const bf16x8 vt = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));                                           \
-    constexpr int set = NH == 8 ? (t) / 2 % 2 : 0;                                                                              \
-    _Pragma("unroll") for (int term = 0; term < kTerms; ++term)                                                                 \
-        st.o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, b[set][term], st.o[t], 0, 0, 0);                                  \
-  }
-  A2ATS_TILE(0) A2ATS_TILE(1) A2ATS_TILE(2) A2ATS_TILE(3) A2ATS_TILE(4) A2ATS_TILE(5) A2ATS_TILE(6) A2ATS_TILE(7)
-#undef A2ATS_TILE
+  to.far[i][lane] = __builtin_bit_cast(uint4, pack8(y));
+  if (NH == 8) to.third[NH == 8 ? i : 0][lane] = __builtin_bit_cast(uint4, pack8(z));
 }
 
-// The queries of far rows as the second operand: bfloat16 terms by truncation.
-template <int NH>
-struct FarQuery {
-  bf16x8 q[4], q2[NH == 8 ? 4 : 1];   // (eight heads: the third term, in the first column of a head)
-  // Elements 32 * lane row + 0 .. 31 of the column's head.
-  __device__ __forceinline__ void set(const float (&x)[32], int term, bool active) {
-    const uint32_t cut1 = term >= 1 ? 0xffff0000u : 0u, cut2 = term >= 2 ? 0xffff0000u : 0u;
-    const uint32_t keep = active && term < 3 ? ~0u : 0u;
+// The first of the eight elements of either half that a lane row has of a turned row; the next eight are 16 on.
+__device__ __forceinline__ int turned_from(int lrow) { return 32 * (lrow & 1) + 8 * (lrow >> 1); }
+
+// Slice i of the window's queries (0, 1: eight elements of the lower half each, 2, 3: of the upper one), as float16 terms of x 2^(8 - e),
+// |x| < 2^e for all of the head: x = 2^(e - 8) (t0 + t1 + t2) but for 2^-33 of 2^e (half the least float16) and, for eight heads with their
+// two terms, 2^-23 of x.  e >= -97: what is below 2^-30 of that is below the least normal number.
+template <typename T, int NH>
+__device__ __forceinline__ void put_win_queries(const T* from, int i, bool active, int lane, Queries<NH>& to) {
+  const int term = Layout<NH>::q_term(lane & 15), at = turned_from(lane >> 4);
+  float big = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float y[8], z[8];
+  for (int j = 0; j < 4; ++j) {
+    float x[8];
+    load8(from + at + 16 * (j & 1) + kD / 2 * (j >> 1), x);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        y[e] = x[8 * i + e];
-        z[e] = lower_part(lower_part(y[e]));
-        z[e] = __uint_as_float(__float_as_uint(z[e]) & (term == 0 ? keep : 0u));
-        y[e] -= __uint_as_float(__float_as_uint(y[e]) & cut1);
-        if (NH != 8) y[e] -= __uint_as_float(__float_as_uint(y[e]) & cut2);
-        y[e] = __uint_as_float(__float_as_uint(y[e]) & keep);
-      }
-      q[i] = pack8(y);
-      if constexpr (NH == 8) q2[i] = pack8(z);
-    }
+    for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(x[e]));   // (a NaN stays one in its own terms)
   }
-  // Products of a tile's keys (32 elements of row `column`) with the queries: rows 4 * lane row + i.
-  __device__ __forceinline__ f32x4 dot(const uint4& k, float scale) const {
-    const uint32_t kw[4] = {k.x, k.y, k.z, k.w};
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  big = rows_max(big) * kLogit;
+  const int e0 = max((int)(__float_as_uint(big) >> 23) - 126, -97);
+  const float down = ldexpf(active && term < 3 ? 1.f : 0.f, 8 - e0);
+  const float less1 = term >= 1 ? 1.f : 0.f, less2 = term >= 2 ? 1.f : 0.f;
+  float y[8];
+  load8(from + at + 16 * (i & 1) + kD / 2 * (i >> 1), y);
+  f16x8 q;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+  for (int e = 0; e < 8; ++e) {
+    float z = y[e] * kLogit * down;
+    z -= less1 * (float)(_Float16)z;
+    if (NH != 8) z -= less2 * (float)(_Float16)z;
+    q[e] = (_Float16)z;
+  }
+  to.win[i][lane] = __builtin_bit_cast(uint4, q);
+  if (i == 0) to.win_scale[lane] = big < INFINITY ? ldexpf(1.f, e0 - 8) : __uint_as_float(0x7fc00000u);
+}
+
+// Byte `at` of row r.  PAGED: of a pool, which may have more than 2^32 bytes; otherwise of a sequence and KV head, at most 2^20 rows.
+template <bool PAGED>
+__device__ __forceinline__ const uint8_t* row_byte(const uint8_t* rows, uint32_t r, int at) {
+  if (PAGED) return rows + (size_t)r * kKv4RowBytes + at;
+  return rows + (r * kKv4RowBytes + (uint32_t)at);
+}
+// A unit's keys or values as they come from memory (`at`: where in a row): 16 bytes of row `column` of each tile, by lane row.  Values by words
+// of the rows that a lane needs would be four times as many requests: 65 instead of 56 us for the rows of 32 x 28 heads.
+template <bool PAGED>
+__device__ __forceinline__ void load_rows(const uint8_t* cache, const uint32_t* rows, int at, int lane, i32x4 (&x)[4]) {
+#pragma unroll
+  for (int t = 0; t < 4; ++t) x[t] = *(const i32x4*)row_byte<PAGED>(cache, rows[t * 16 + (lane & 15)], at + (lane >> 4) * 16);
+}
+
+// Products of the queries with a unit's far keys: row `column` of tile t in dot[t].
+template <int NH>
+__device__ __forceinline__ void far_dots(const i32x4 (&k)[4], const uint8_t* scales, int lane, const Queries<NH>& queries, f32x4 (&dot)[4]) {
+  float scale[4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    scale[t] = kv4_scale(scales[(t * 16 + (lane & 15)) * 4 + (lane >> 4)]);
+    dot[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bf16x8 q = __builtin_bit_cast(bf16x8, queries.far[i][lane]);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
       uint32_t w[4];
-#define A2ATS_PAIR(e) w[e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(kw[i], scale, e));
+#define A2ATS_PAIR(e) w[e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((uint32_t)k[t][i], scale[t], e));
       A2ATS_PAIR(0) A2ATS_PAIR(1) A2ATS_PAIR(2) A2ATS_PAIR(3)
 #undef A2ATS_PAIR
       const bf16x8 k8 = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, q[i], acc, 0, 0, 0);
-      if constexpr (NH == 8) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, q2[i], acc, 0, 0, 0);
+      dot[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, k8, dot[t], 0, 0, 0);
+      if (NH == 8)
+        dot[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, queries.third[NH == 8 ? i : 0][lane]), k8, dot[t], 0, 0, 0);
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) acc[i] = Columns<NH>::sum(acc[i]);
-    return acc;
   }
-};
+}
 
-// Products of a tile's window keys (elements 16 * lane row + 0 .. 15 of either half of row `column`, whose groups have the scales
-// s_lower and s_upper), turned back by the row's angles, with the queries' float16 terms.
-__device__ __forceinline__ f32x4 turned_dot(const uint4& k, float s_lower, float s_upper, const float (&cs)[16], const float (&sn)[16],
-                                            const f16x8 (&q)[4]) {
-  const uint32_t lw[2] = {k.x, k.y}, uw[2] = {k.z, k.w};
+// The same of a tile's window keys, turned back by the row's angles (cs, sn: its rows of the tables).  The other half of an element is two
+// lane rows on, so these lane rows exchange words: the first two have words 0 and 2 of both, the others 1 and 3.  sc: the row's scale bytes;
+// the products are relative to the largest.
+template <int NH>
+__device__ __forceinline__ f32x4 turned_dot(const i32x4& k, uint32_t sc, const float* cs_row, const float* sn_row, int lane,
+                                            const Queries<NH>& queries) {
+  const int lrow = lane >> 4;
+  uint32_t most = 0;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) most = max(most, (sc >> (8 * g)) & 255u);
+  const int down = 127 - (int)most;
+  const uint32_t lower_byte = (sc >> (8 * (lrow & 1))) & 255u, upper_byte = (sc >> (16 + 8 * (lrow & 1))) & 255u;
+  const float s_lower = kv4_scale((uint32_t)max((int)lower_byte + down, 0)), s_upper = kv4_scale((uint32_t)max((int)upper_byte + down, 0));
+  float cs[2][8], sn[2][8];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    load8(cs_row + turned_from(lrow) + 16 * i, cs[i]);
+    load8(sn_row + turned_from(lrow) + 16 * i, sn[i]);
+  }
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < 2; ++i) {   // eight pairs of elements
+    const auto words = __builtin_amdgcn_permlane32_swap((uint32_t)k[2 * i], (uint32_t)k[2 * i + 1], false, false);
     float lower[8], upper[8];
 #define A2ATS_PAIR(e)                                                                          \
   {                                                                                            \
-    const auto dl = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(lw[i], s_lower, e);               \
-    const auto du = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(uw[i], s_upper, e);               \
+    const auto dl = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(words[0], s_lower, e);            \
+    const auto du = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(words[1], s_upper, e);            \
     _Pragma("unroll") for (int j = 0; j < 2; ++j) {                                            \
-      lower[2 * e + j] = dl[j] * cs[8 * i + 2 * e + j] + du[j] * sn[8 * i + 2 * e + j];        \
-      upper[2 * e + j] = du[j] * cs[8 * i + 2 * e + j] - dl[j] * sn[8 * i + 2 * e + j];        \
+      lower[2 * e + j] = dl[j] * cs[i][2 * e + j] + du[j] * sn[i][2 * e + j];                  \
+      upper[2 * e + j] = du[j] * cs[i][2 * e + j] - dl[j] * sn[i][2 * e + j];                  \
     }                                                                                          \
   }
     A2ATS_PAIR(0) A2ATS_PAIR(1) A2ATS_PAIR(2) A2ATS_PAIR(3)
 #undef A2ATS_PAIR
-    auto terms = [&](const float (&x)[8], const f16x8& qt) {
+    auto terms = [&](const float (&x)[8], const uint4& query) {
+      const f16x8 qt = __builtin_bit_cast(f16x8, query);
       uint32_t hi[4], lo[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -282,26 +231,80 @@ __device__ __forceinline__ f32x4 turned_dot(const uint4& k, float s_lower, float
         hi[j] = f16_bits(h);
         lo[j] = f16_bits(f16_pair(x[2 * j] - (float)h[0], x[2 * j + 1] - (float)h[1]));
       }
-      acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, make_uint4(hi[0], hi[1], hi[2], hi[3])), qt, acc, 0, 0, 0);
-      acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, make_uint4(lo[0], lo[1], lo[2], lo[3])), qt, acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(qt, __builtin_bit_cast(f16x8, make_uint4(hi[0], hi[1], hi[2], hi[3])), acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(qt, __builtin_bit_cast(f16x8, make_uint4(lo[0], lo[1], lo[2], lo[3])), acc, 0, 0, 0);
     };
-    terms(lower, q[i]);
-    terms(upper, q[2 + i]);
+    terms(lower, queries.win[i][lane]);
+    terms(upper, queries.win[2 + i][lane]);
   }
+  __builtin_amdgcn_sched_barrier(0);   // (several tiles at once would not fit the registers)
   return acc;
 }
 
+// The bits of a where the mask has ones, else those of b.
+__device__ __forceinline__ uint32_t select_bits(uint32_t mask, uint32_t a, uint32_t b) { return (mask & a) | (~mask & b); }
+
+// 32 rows' values, of which a lane has a word (two dimensions of each group) of the rows 4 e + lane row, e = 0 .. 7, so that what the lanes
+// of a wave read at a time is in one piece of LDS.  Two rows' words together: byte g of even[i] has the first of the two dimensions of group g
+// of the rows e = 2 i and 2 i + 1, of odd[i] the second; the lower half of a byte is the first row's.
+struct Values {
+  uint32_t even[4], odd[4];
+  __device__ __forceinline__ Values(const uint32_t* v) {   // word `column` of row `lane row`
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t a = v[8 * i * 16], c = v[(8 * i + 4) * 16];
+      even[i] = select_bits(0x0f0f0f0fu, a, c << 4);
+      odd[i] = select_bits(0x0f0f0f0fu, a >> 4, c);
+    }
+  }
+};
+// Where a row's weight is among those of a column: row 32 h + 4 e + r is element e of lane row r, of half h.
+__device__ __forceinline__ int weight_at(int row) { return (row & 32) | (row & 3) << 3 | (row >> 2 & 7); }
+
+// Their products with the weights (columns of LDS; one head: a term a column, else three terms), added to the outputs: o[t][i] is
+// dimension 32 (t / 2) + 2 (4 * lane row + i) + t % 2, in the columns of group t / 2.  SET: eight heads, groups SET and 2 + SET.
+template <int NH, int SET>
+__device__ __forceinline__ void absorb(const Values& v, const uint16_t* weights, f32x4 (&o)[8]) {
+  constexpr int kTerms = NH == 1 ? 1 : 3;
+  bf16x8 b[kTerms];
+#pragma unroll
+  for (int term = 0; term < kTerms; ++term) b[term] = __builtin_bit_cast(bf16x8, *(const uint4*)(weights + term * 16 * kUnit));
+#define A2ATS_TILE(t)                                                                                                                 \
+  if (NH != 8 || (t) / 2 % 2 == SET) {                                                                                                \
+    uint32_t w[4];                                                                                                                    \
+    _Pragma("unroll") for (int i = 0; i < 4; ++i)                                                                                     \
+        w[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((t) & 1 ? v.odd[i] : v.even[i], 1.f, (t) / 2)); \
+    const bf16x8 vt = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));                                                 \
+    _Pragma("unroll") for (int term = 0; term < kTerms; ++term)                                                                       \
+        o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, b[term], o[t], 0, 0, 0);                                                   \
+  }
+  A2ATS_TILE(0) A2ATS_TILE(1) A2ATS_TILE(2) A2ATS_TILE(3) A2ATS_TILE(4) A2ATS_TILE(5) A2ATS_TILE(6) A2ATS_TILE(7)
+#undef A2ATS_TILE
+}
+
+// Over the 16 lanes of a lane row, in each of them.
+template <typename F>
+__device__ __forceinline__ float over_columns(float v, F f) {
+  v = f(v, dpp<0xB1>(v));    // quad_perm [1,0,3,2]
+  v = f(v, dpp<0x4E>(v));    // quad_perm [2,3,0,1]
+  v = f(v, dpp<0x124>(v));   // row_ror:4
+  return f(v, dpp<0x128>(v));
+}
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
+
 // NH: heads that attend the same rows, one, or the G of a KV head if the selection is shared, padded to 4 or 8.
-template <typename T, int NH>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_kv4_kernel(Attn4Args a) {
+template <typename T, int NH, bool PAGED>
+__global__ __launch_bounds__(kThreads, NH == 1 ? 4 : 2) void attn_kv4_kernel(Attn4Args a) {
+  typedef Layout<NH> L;
   __shared__ __align__(16) union {
     struct {
-      PairPlaces far[kWaves][2], win[kWaves];
-    } places;
+      Queries<NH> queries;
+      WaveMemory<NH> wave[kWaves];
+    } in;
     float o[kWaves][NH][kD];
   } s;
   __shared__ float s_m[kWaves][NH], s_l[kWaves][NH];
-  typedef Columns<NH> C;
 
   // All workgroups of a KV head run on one XCD, whose L2 then serves the rows that its heads have in common.
   const int G = a.group, nh = a.shared ? G : 1, per = a.shared ? a.parts : a.parts * G;
@@ -315,231 +318,272 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, lrow = lane >> 4;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int32_t* idx = a.sel_idx + (size_t)sel * a.n_sel;
+  const size_t first_row = PAGED ? 0 : ((size_t)prob * (size_t)blocks.blocks_per_seq) << blocks.shift;
+  const uint8_t *rows = a.cache.rows + first_row * kKv4RowBytes, *scales = a.cache.scales + first_row * kKv4ScaleBytes;
 
-  // This part's share of the far rows: row t is sink t, then row t - n_sink of the selection.  Places without a row are left
-  // out: what a part has to fetch first does not depend on the sequence's length.
+  // The part's share of the far rows (row t is sink t, then row t - n_sink of the selection) and of the window's is dealt out to the waves by
+  // tiles, those of the window first.  It goes by what the call allows, not by the sequence: what has to be fetched first does not
+  // wait for its length.
   const int n_sink = min(a.n_sink, a.ctx_len);
-  const int f0 = part * a.far_share;
-  auto unit_of = [&](int t) {   // (clamped: requested before it is known to count)
-    return a.n_sel > 0 ? idx[min(max(t - n_sink, 0) >> a.sel_shift, a.n_sel - 1)] : 0;
+  const int win_tiles = (a.win_share + 16 * kWaves - 1) / (16 * kWaves), far_tiles = (a.far_share + 16 * kWaves - 1) / (16 * kWaves);
+  const int f0 = part * a.far_share + (wv * far_tiles - win_tiles) * 16, w0 = part * a.win_share + wv * win_tiles * 16;
+  auto unit_of = [&](int u) {   // (clamped: requested before it is known to count)
+    return a.n_sel > 0 ? idx[min(max(f0 + u * kUnit + lane - n_sink, 0) >> a.sel_shift, a.n_sel - 1)] : 0;
   };
-
+  int index = unit_of(0);
   const SeqRange sr = seq_range(a.ctx_len, a.seq_lens, b, a.window, a.n_sink, 0);
-  const int shift = blocks.shift, blk = 1 << shift;
   const int cnt = min(max(a.sel_count[sel], 0), a.n_sel);
-  const int f1 = min(f0 + a.far_share, n_sink + (cnt << a.sel_shift));
-  // ... and of the window's rows, [w0, w1).
-  const int w0 = sr.win_start + part * a.win_share, w1 = max(w0, min(w0 + a.win_share, sr.n));
-  const int n_far = f1 > f0 && sr.n > 0 ? (f1 - f0 + kPair - 1) / kPair : 0, n_win = (w1 - w0 + kPair - 1) / kPair;
-  // Wave by wave, the pairs win_first, win_first + kWaves, .. of the window, and of the far rows a stretch, so that all waves have
-  // about as much to do: a pair of the window is as much as two others.  Which wave of the SIMDs is the first goes by the
-  // workgroup (the waves with the window would else be on one SIMD in all workgroups of a CU).
-  const int win_first = (wv + (int)(blockIdx.x >> 3) + (int)(blockIdx.x >> 8)) & (kWaves - 1);
-  const int quota = (2 * n_win + n_far + kWaves - 1) / kWaves;
-  int far_first = 0, far_end = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    const int take = max(quota - 2 * ((n_win - w + kWaves - 1) / kWaves), 0);   // (n_win + kWaves > w)
-    far_first += w < win_first ? take : 0;
-    far_end += w <= win_first ? take : 0;
-  }
-  far_first = min(far_first, n_far);
-  far_end = min(far_end, n_far);
-  // Lane l places row l % 32 of a pair (l < 32) or of the next one.
-  auto far_row = [&](int pair) { return f0 + pair * kPair + lane; };
-  int unit = unit_of(far_row(far_first));
+  const int f1 = min(min((part + 1) * a.far_share, f0 + (win_tiles + far_tiles) * 16), n_sink + (cnt << a.sel_shift));
+  const int w1 = min(sr.n, sr.win_start + (part + 1) * a.win_share);
+  // Units with a row: of the window, or of far rows.
+  const int win_units = min(max(w1 - sr.win_start - w0 + kUnit - 1, 0) / kUnit, (win_tiles + 3) / 4);
+  const int units = sr.n > 0 ? max(win_units, (max(f1 - f0, 0) + kUnit - 1) / kUnit * (f1 > f0 + win_tiles * 16)) : 0;
 
-  // This lane's column: a head.
-  const int hd = C::head(col);
-  const bool active = hd < nh;
-  const size_t q_at = (size_t)(head + min(hd, nh - 1)) * kD;
-
-  // Where this lane's row is, and its scales, which are requested here and put beside it by put_scales.
+  WaveMemory<NH>& wm = s.in.wave[wv];
+  // Lane l places row l of a unit, and requests its scales.
   struct Place {
-    size_t at;
     uint2 sc;
     bool in;
   };
-  auto place = [&](PairPlaces& to, int j, bool in) {   // row j of the sequence
+  auto place = [&](uint32_t* to, int u) {
+    const int tile = 4 * u + lrow, t = f0 + u * kUnit + lane;
+    bool in;
+    int j = t;
+    if (tile < win_tiles) {
+      j = sr.win_start + w0 + u * kUnit + lane;
+      in = j < w1;
+    } else {
+      in = t < f1 && u < units;
+      if (t >= n_sink) {
+        in = in && index >= 0 && index <= (sr.n - 1) >> a.sel_shift;   // (an index from elsewhere must not leave the cache)
+        j = in ? (index << a.sel_shift) + ((t - n_sink) & ((1 << a.sel_shift) - 1)) : 0;
+        in = in && j >= sr.sink_end && j < sr.win_start;
+      } else {
+        in = in && t < sr.sink_end;
+      }
+    }
     Place pc;
     pc.in = in;
     j = in ? j : 0;   // (a place without a row: the sequence's first one, which has been written and counts for nothing)
-    pc.at = (block_at(blocks, b, kv, j >> shift) << shift) + (size_t)(j & (blk - 1));
+    uint32_t at = (uint32_t)j;
+    if (PAGED) at = (uint32_t)((block_at(blocks, b, kv, j >> blocks.shift) << blocks.shift) + (size_t)(j & ((1 << blocks.shift) - 1)));
     wave_exchange();
-    to.row[lane] = (uint32_t)pc.at;
+    to[lane] = at;
     wave_exchange();
+    pc.sc = *(const uint2*)(PAGED ? scales + (size_t)at * kKv4ScaleBytes : scales + at * (uint32_t)kKv4ScaleBytes);
     return pc;
   };
-  auto get_scales = [&](Place& pc) { pc.sc = *(const uint2*)(a.cache.scales + pc.at * kKv4ScaleBytes); };
-  // turned: products are relative to the row's largest scale.
-  auto put_scales = [&](PairPlaces& to, const Place& pc, bool turned) {
+
+  // A wave has one unit in flight: the next one's rows are requested when a unit's keys have become products, and its values are in LDS.  Requests are made whether there is a next unit or not (then for the sequence's first row): the wait for what a unit
+  // needs would be one for all requests if it were not known how many come after it.
+  float m[L::kHeads], l[L::kHeads];   // running maximum of a head, and the sum of the lane's own weights
+  f32x4 o[8];
+  i32x4 k[4], v[4];
+  Place at, next;
+  if (units > 0) {
+    at = place(wm.row[0], 0);
+    load_rows<PAGED>(rows, wm.row[0], 0, lane, k);
+    load_rows<PAGED>(rows, wm.row[0], kKv4Half, lane, v);
+    index = unit_of(1);
+  }
+  {
+    const size_t q_at = (size_t)(head + min(L::q_head(col), nh - 1)) * kD;
+    const bool active = L::q_head(col) < nh;
+    put_far_queries<NH>(a.q_rot + q_at + lrow * 32, wv, active, lane, s.in.queries);
+    if (a.window > 0) put_win_queries<T, NH>((const T*)a.q + q_at, wv, active, lane, s.in.queries);
+  }
+  if (NH == 1) wm.weights[NH == 1 ? 12 : 0][lane] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int h = 0; h < L::kHeads; ++h) {
+    m[h] = kNone;
+    l[h] = 0.f;
+  }
+#pragma unroll
+  for (int t = 0; t < 8; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const uint16_t* my_weights = wm.weights[NH == 1 ? min(col, 12) : col] + lrow * 8;
+
+#pragma unroll 1
+  for (int u = 0; u < units; ++u) {
+    // The scales of this unit's rows, for the lanes that have them as keys, and the values, from where they are read again by rows.
     uint32_t most = 0;
 #pragma unroll
-    for (int g = 0; g < 4; ++g) most = max(most, (pc.sc.x >> (8 * g)) & 255u);
-    const float ks = turned ? kv4_scale(most) : 1.f;
+    for (int g = 0; g < 4; ++g) most = max(most, (at.sc.x >> (8 * g)) & 255u);
+    const float ks = most == 255u ? __uint_as_float(0x7fc00000u) : 1.f;
     wave_exchange();
-    to.ksc[lane] = pc.sc.x;
-    to.ks[lane] = most == 255u ? __uint_as_float(0x7fc00000u) : ks;
-    to.none[lane] = pc.in ? 0u : ~0u;
+    wm.ksc[lane] = at.sc.x;
+    if (NH != 1) {
+      wm.vsc[NH == 1 ? 0 : lane] = at.sc.y;
+      wm.ks[NH == 1 ? 0 : lane] = at.in ? ks : -1.f;
+    }
+    if (4 * u < win_tiles) wm.win_ks[lane] = kv4_scale(most);
 #pragma unroll
-    for (int g = 0; g < 4; ++g) to.vs[g][lane] = pc.in ? kv4_scale((pc.sc.y >> (8 * g)) & 255u) : 0.f;
+    for (int t = 0; t < 4; ++t) wm.values[t * 16 + col][lrow] = v[t];
     wave_exchange();
-  };
-  PairPlaces &wp = s.places.win[wv], *fp = s.places.far[wv];
-  auto place_far = [&](PairPlaces& to, int pair) {   // this pair and the next one
-    const int t = far_row(pair);
-    bool in = t < f1;
-    int j = t;
-    if (t >= n_sink) {
-      in = in && unit >= 0 && unit <= (sr.n - 1) >> a.sel_shift;   // (an index from elsewhere must not leave the cache)
-      j = in ? (unit << a.sel_shift) + ((t - n_sink) & ((1 << a.sel_shift) - 1)) : 0;
-      in = in && j >= sr.sink_end && j < sr.win_start;
+    uint32_t* next_rows = wm.row[(u & 1) ^ 1];
+    next = place(next_rows, u + 1);
+    index = unit_of(u + 2);
+
+    f32x4 dot[4];
+    far_dots<NH>(k, (const uint8_t*)wm.ksc, lane, s.in.queries, dot);
+    if (4 * u < win_tiles) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        if (4 * u + t < win_tiles) {
+          const int delta = min(max(sr.n - 1 - (sr.win_start + w0 + u * kUnit + t * 16 + col), 0), a.window - 1);
+          dot[t] = turned_dot<NH>(k[t], wm.ksc[t * 16 + col], a.cos_win + (size_t)delta * (kD / 2), a.sin_win + (size_t)delta * (kD / 2), lane,
+                                  s.in.queries);
+          // (of the query's row 4 * lane row: the terms of a head have the same)
+          dot[t] *= wm.win_ks[t * 16 + col];
+          const float4 qs = *(const float4*)(s.in.queries.win_scale + 4 * lrow);
+          dot[t] = f32x4{dot[t][0] * qs.x, dot[t][1] * qs.y, dot[t][2] * qs.z, dot[t][3] * qs.w};
+        }
+      }
+    }
+    load_rows<PAGED>(rows, next_rows, 0, lane, k);
+    load_rows<PAGED>(rows, next_rows, kKv4Half, lane, v);
+
+    // Logits: one head, of the lane's own row; else of row `column` of each tile, of the lane row's heads.
+    float p[L::kOwn];
+    if constexpr (NH == 1) {
+      float lg[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) lg[t] = dot[t][0] + dot[t][1] + dot[t][2];
+      const float x = (lrow & 2) ? ((lrow & 1) ? lg[3] : lg[2]) : ((lrow & 1) ? lg[1] : lg[0]);
+      p[0] = at.in ? x * ks : -INFINITY;
     } else {
-      in = in && t < sr.sink_end;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const float kt = wm.ks[NH == 1 ? 0 : t * 16 + col];
+#pragma unroll
+        for (int h = 0; h < L::kHeads; ++h) {
+          const float x = NH == 8 ? dot[t][2 * h] + dot[t][2 * h + 1] : dot[t][0] + dot[t][1] + dot[t][2];
+          p[t * L::kHeads + h] = kt < 0.f ? -INFINITY : x * kt;
+        }
+      }
     }
-    return place(to, j, in);
-  };
-  auto place_win = [&](int pair) {
-    const int j = w0 + pair * kPair + lane;
-    return place(wp, j, lane < kPair && j < w1);
-  };
+    float mn[L::kHeads];
+    bool rise = false;
+#pragma unroll
+    for (int h = 0; h < L::kHeads; ++h) {
+      float mx = p[h];
+#pragma unroll
+      for (int i = h + L::kHeads; i < L::kOwn; i += L::kHeads) mx = fmaxf(mx, p[i]);
+      mx = over_columns(mx, larger);
+      if (NH == 1) mx = rows_max(mx);
+      mn[h] = fmaxf(m[h], mx);
+      rise = rise || mn[h] > m[h];
+    }
+    if (__builtin_amdgcn_ballot_w64(rise)) {
+      float alpha;
+      if constexpr (NH == 1) {
+        alpha = power(m[0] - mn[0]);
+        l[0] *= alpha;
+      } else {   // from the lane rows that have a head's logits to the columns that have its output
+        wave_exchange();
+#pragma unroll
+        for (int h = 0; h < L::kHeads; ++h) {
+          const float f = power(m[h] - mn[h]);
+          l[h] *= f;
+          if (col == 0) wm.alpha[lrow * L::kHeads + h] = f;
+        }
+        wave_exchange();
+        alpha = wm.alpha[L::col_head(col)];
+      }
+#pragma unroll
+      for (int t = 0; t < 8; ++t) o[t] *= alpha;
+#pragma unroll
+      for (int h = 0; h < L::kHeads; ++h) m[h] = mn[h];
+    }
+#pragma unroll
+    for (int i = 0; i < L::kOwn; ++i) {
+      p[i] = power(p[i] - mn[i % L::kHeads]);
+      l[i % L::kHeads] += p[i];
+    }
 
-  // A wave takes its pairs of the window, then those of the far rows, two of which are in flight at a time: a pair's keys and
-  // values are requested when those of the pair two before it have been used.  What does not depend on other loads comes first.
-  const int far_n = far_end - far_first;
-  const bool has_win = win_first < n_win;
-  WaveState st;
-  PairRows pa, pc;
-  Place far_place;
-  st.m = kNone;
-  st.l = 0.f;
+    // Weights times the scales of the groups, as three bfloat16 terms, into the columns of the second product.
+    auto put = [&](float x, int c0, int step, int row) {
 #pragma unroll
-  for (int t = 0; t < 8; ++t) st.o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const uint8_t* rows = a.cache.rows;
-  if (has_win) {
-    float x[32];
-    load_elems<16>((const T*)a.q + q_at + lrow * 16, x);
-    load_elems<16>((const T*)a.q + q_at + kD / 2 + lrow * 16, x + 16);
-    Place win_place = place_win(win_first);
-    if (far_n > 0) far_place = place_far(fp[0], far_first);
-    get_scales(win_place);
-    if (far_n > 0) get_scales(far_place);
-    load_turned_pair(rows, wp.row, col, lrow, pc);
-    if (far_n > 0) load_pair(rows, fp[0].row, col, lrow, pa);
-    f16x8 qw[4];
-    to_logits(x);
-    const float ww = query_terms<NH == 8 ? 8 : 4>(x, C::q_term(col), active, qw);
-    if (far_n > 0) put_scales(fp[0], far_place, false);
-#pragma unroll 1
-    for (int pair = win_first; pair < n_win; pair += kWaves) {
-      put_scales(wp, win_place, true);
-      f32x4 dot[2];
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int delta = min(max(sr.n - 1 - (w0 + pair * kPair + t * 16 + col), 0), a.window - 1);
-        float cs[16], sn[16];
-        load_elems<16>(a.cos_win + (size_t)delta * (kD / 2) + lrow * 16, cs);
-        load_elems<16>(a.sin_win + (size_t)delta * (kD / 2) + lrow * 16, sn);
-        const uint32_t sc = wp.ksc[t * 16 + col];
-        uint32_t most = 0;
-#pragma unroll
-        for (int g = 0; g < 4; ++g) most = max(most, (sc >> (8 * g)) & 255u);
-        const int down = 127 - (int)most;
-        const uint32_t lower = (sc >> (8 * (lrow >> 1))) & 255u, upper = (sc >> (16 + 8 * (lrow >> 1))) & 255u;
-        const f32x4 acc = turned_dot(pc.k[t], kv4_scale((uint32_t)max((int)lower + down, 0)),
-                                     kv4_scale((uint32_t)max((int)upper + down, 0)), cs, sn, qw);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) dot[t][i] = C::sum(acc[i]) * ww;
+      for (int term = 0; term < 3; ++term) {
+        wm.weights[c0 + term * step][weight_at(row)] = upper_half(x);
+        x = lower_part(x);
       }
-      float w[8];
-      pair_weights(dot, wp, 0, lrow, st, w);
-      absorb_values<NH>(w, wp, 0, col, lrow, pc, st);
-      if (pair + kWaves < n_win) {
-        win_place = place_win(pair + kWaves);
-        get_scales(win_place);
-        load_turned_pair(rows, wp.row, col, lrow, pc);
-      }
-    }
-    if (far_n > 1) load_pair(rows, fp[0].row + kPair, col, lrow, pc);
-  }
-  if (far_n > 0) {
-    FarQuery<NH> fq;
-    float x[32];
-    load_elems<32>(a.q_rot + q_at + lrow * 32, x);
-    if (!has_win) {
-      far_place = place_far(fp[0], far_first);
-      get_scales(far_place);
-      load_pair(rows, fp[0].row, col, lrow, pa);
-      if (far_n > 1) load_pair(rows, fp[0].row + kPair, col, lrow, pc);
-      put_scales(fp[0], far_place, false);
-    }
-    if (far_n > 2) unit = unit_of(far_row(far_first + 2));
-    to_logits(x);
-    fq.set(x, C::q_term(col), active);
-    auto use = [&](const PairRows& p, const PairPlaces& pl, int first) {
-      f32x4 dot[2];
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-        dot[t] = fq.dot(p.k[t], kv4_scale(((const uint8_t*)(pl.ksc + first + t * 16 + col))[lrow]));
-      float w[8];
-      pair_weights(dot, pl, first, lrow, st, w);
-      absorb_values<NH>(w, pl, first, col, lrow, p, st);
     };
-    int buf = 0;
-#pragma unroll 1
-    for (int i = 0; i < far_n; i += 2) {
-      const PairPlaces& pl = fp[buf];
-      PairPlaces& next = fp[buf ^ 1];
-      const bool more = i + 2 < far_n;
-      if (more) {
-        far_place = place_far(next, far_first + i + 2);
-        get_scales(far_place);
-        if (i + 4 < far_n) unit = unit_of(far_row(far_first + i + 4));
+    const uint32_t* words = (const uint32_t*)&wm.values[lrow][0] + col;
+    if constexpr (NH == 1) {
+      const uint32_t vsc = at.in ? at.sc.y : 0u;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) put(p[0] * kv4_scale((vsc >> (8 * g)) & 255u), g, 4, lane);
+      wave_exchange();
+      absorb<NH, 0>(Values(words), my_weights, o);
+      absorb<NH, 0>(Values(words + kUnit / 2 * 16), my_weights + kUnit / 2, o);
+    } else {
+#pragma unroll
+      for (int set = 0; set < (NH == 8 ? 2 : 1); ++set) {
+        wave_exchange();
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const uint32_t vsc = wm.ks[NH == 1 ? 0 : t * 16 + col] < 0.f ? 0u : wm.vsc[NH == 1 ? 0 : t * 16 + col];
+#pragma unroll
+          for (int h = 0; h < L::kHeads; ++h)
+#pragma unroll
+            for (int g = 0; g < (NH == 8 ? 2 : 4); ++g)
+              put(p[t * L::kHeads + h] * kv4_scale((vsc >> (8 * (NH == 8 ? 2 * g + set : g))) & 255u),
+                  NH == 8 ? 2 * (2 * lrow + h) + g : 4 * lrow + g, 16, t * 16 + col);
+        }
+        wave_exchange();
+        if (set == 0) {
+          absorb<NH, 0>(Values(words), my_weights, o);
+          absorb<NH, 0>(Values(words + kUnit / 2 * 16), my_weights + kUnit / 2, o);
+        } else {
+          absorb<NH, 1>(Values(words), my_weights, o);
+          absorb<NH, 1>(Values(words + kUnit / 2 * 16), my_weights + kUnit / 2, o);
+        }
       }
-      use(pa, pl, 0);
-      if (more) load_pair(rows, next.row, col, lrow, pa);
-      if (i + 1 < far_n) use(pc, pl, kPair);
-      if (i + 3 < far_n) load_pair(rows, next.row + kPair, col, lrow, pc);
-      if (more) put_scales(next, far_place, false);
-      buf ^= 1;
     }
+    at = next;
   }
-  __syncthreads();   // (the places are written again, with the outputs)
+  __syncthreads();   // (the waves' memory is written again, with the outputs)
 
-  // The terms of a weight are added up, each tile's from the columns of its own group, and the waves merged.
-  const float l_all = rows_sum(st.l);
+  // The terms of a weight are added up (one head), each tile's from the columns of its own group, and the waves merged.
 #pragma unroll
   for (int t = 0; t < 8; ++t)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float o = NH == 1 ? head_sum<4>(st.o[t][i]) : st.o[t][i];
-      if (NH == 1 ? col == t / 2 : C::group(col) == (NH == 8 ? t / 4 : t / 2))
-        s.o[wv][hd][32 * (t / 2) + 2 * (4 * lrow + i) + t % 2] = o;
+      const float x = NH == 1 ? head_sum<4>(o[t][i]) : o[t][i];
+      const int g = t / 2;
+      if (NH == 1 ? col == g : (NH == 4 ? (col & 3) == g : (col & 1) == g / 2))
+        s.o[wv][L::col_head(col)][32 * g + 2 * (4 * lrow + i) + t % 2] = x;
     }
-  if (lane < NH) {
-    s_m[wv][lane] = st.m;
-    s_l[wv][lane] = l_all;
+#pragma unroll
+  for (int h = 0; h < L::kHeads; ++h) {
+    float all = over_columns(l[h], sum_of);
+    if (NH == 1) all = rows_sum(all);
+    if (NH == 1 ? lane == 0 : col == 0) {
+      s_m[wv][NH == 1 ? 0 : lrow * L::kHeads + h] = m[h];
+      s_l[wv][NH == 1 ? 0 : lrow * L::kHeads + h] = all;
+    }
   }
   __syncthreads();
   for (int i = tid; i < nh * kD; i += kThreads) {
     const int g = i / kD, d = i % kD;
-    float m = s_m[0][g], l = 0.f, o = 0.f;
+    float mx = s_m[0][g], ls = 0.f, x = 0.f;
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) m = fmaxf(m, s_m[w][g]);
+    for (int w = 1; w < kWaves; ++w) mx = fmaxf(mx, s_m[w][g]);
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const float f = power(s_m[w][g] - m);
-      l += s_l[w][g] * f;
-      o += s.o[w][g][d] * f;
+      const float f = power(s_m[w][g] - mx);
+      ls += s_l[w][g] * f;
+      x += s.o[w][g][d] * f;
     }
     if (a.parts == 1) {
-      store_elem((T*)a.out + (size_t)(head + g) * kD + d, l == 0.f ? 0.f : o / l);
+      store_elem((T*)a.out + (size_t)(head + g) * kD + d, ls == 0.f ? 0.f : x / ls);
     } else {
       float* to = a.partial + ((size_t)(head + g) * a.parts + part) * (kD + 2);
-      to[d] = o;
+      to[d] = x;
       if (d == 0) {
-        to[kD] = m;
-        to[kD + 1] = l;
+        to[kD] = mx;
+        to[kD + 1] = ls;
       }
     }
   }
@@ -560,12 +604,12 @@ Kv4Plan make_kv4_plan(const a2ats_dims& d, long sel_rows, int window, bool share
   return p;
 }
 
-template <typename T>
+template <typename T, bool PAGED>
 static void launch_heads(const Attn4Args& a, long workgroups, hipStream_t stream) {
   const dim3 grid((unsigned)workgroups), block(kThreads);
-  if (!a.shared || a.group == 1) hipLaunchKernelGGL((attn_kv4_kernel<T, 1>), grid, block, 0, stream, a);
-  else if (a.group <= 4) hipLaunchKernelGGL((attn_kv4_kernel<T, 4>), grid, block, 0, stream, a);
-  else hipLaunchKernelGGL((attn_kv4_kernel<T, 8>), grid, block, 0, stream, a);
+  if (!a.shared || a.group == 1) hipLaunchKernelGGL((attn_kv4_kernel<T, 1, PAGED>), grid, block, 0, stream, a);
+  else if (a.group <= 4) hipLaunchKernelGGL((attn_kv4_kernel<T, 4, PAGED>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((attn_kv4_kernel<T, 8, PAGED>), grid, block, 0, stream, a);
 }
 
 hipError_t launch_sparse_attn_kv4(const a2ats_dims& d, const Kv4Cache& m, int kv_dtype, const void* q, const float* q_rot,
@@ -598,8 +642,14 @@ hipError_t launch_sparse_attn_kv4(const a2ats_dims& d, const Kv4Cache& m, int kv
   a.win_share = (int)((win + p.parts - 1) / p.parts);
   a.problems = d.batch * d.n_kv_heads;
   const long workgroups = (long)a.problems * p.parts * (shared ? 1 : a.group);
-  if (kv_dtype == A2ATS_BF16) launch_heads<uint16_t>(a, workgroups, stream);
-  else launch_heads<float>(a, workgroups, stream);
+  const bool paged = m.at.pages != nullptr;
+  if (kv_dtype == A2ATS_BF16) {
+    if (paged) launch_heads<uint16_t, true>(a, workgroups, stream);
+    else launch_heads<uint16_t, false>(a, workgroups, stream);
+  } else {
+    if (paged) launch_heads<float, true>(a, workgroups, stream);
+    else launch_heads<float, false>(a, workgroups, stream);
+  }
   const hipError_t e = hipGetLastError();
   return e != hipSuccess || p.parts == 1 ? e : launch_attn_merge(kv_dtype, (const float*)ws, out, d.batch * d.n_q_heads, p.parts, stream);
 }
