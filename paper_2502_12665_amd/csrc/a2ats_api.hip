@@ -188,9 +188,7 @@ size_t a2ats_workspace_bytes(const a2ats_dims* d, int op, int32_t top_k, int32_t
     }
     case A2ATS_OP_ATTN_KV4: {
       if (top_k < 0 || window < 0) return (size_t)-1;
-      const size_t own = a2ats::make_kv4_plan(*d, top_k, window, false).bytes;
-      const size_t shared = a2ats::make_kv4_plan(*d, top_k, window, true).bytes;
-      return own > shared ? own : shared;
+      return a2ats::kv4_ws_bytes(*d, top_k, window);
     }
     case A2ATS_OP_FIT: return a2ats::fit_ws_bytes(*d);
     case A2ATS_OP_SEED: return a2ats::single_codebook(*d) ? a2ats::kmeanspp_ws_bytes(*d) : (size_t)-1;

@@ -232,6 +232,7 @@ struct Kv4Plan {
   size_t bytes;
 };
 Kv4Plan make_kv4_plan(const a2ats_dims& d, long sel_rows, int window, bool shared);
+size_t kv4_ws_bytes(const a2ats_dims& d, long sel_rows, int window);
 hipError_t launch_sparse_attn_kv4(const a2ats_dims& d, const Kv4Cache& m, int kv_dtype, const void* q, const float* q_rot,
                                   const int32_t* sel_idx, const int32_t* sel_count, int n_sel, int sel_shift, bool shared, int window,
                                   int n_sink, const float* cos_win, const float* sin_win, const int32_t* seq_lens, void* out,

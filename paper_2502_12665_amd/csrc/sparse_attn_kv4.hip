@@ -71,7 +71,7 @@ struct alignas(16) WaveMemory {
   uint32_t ksc[kUnit];                             // scale bytes of the keys
   uint32_t vsc[NH == 1 ? 1 : kUnit];               // ... of the values (one head: a lane has its own row's)
   float ks[NH == 1 ? 1 : kUnit];                   // 1, or NaN for a key that is; -1 without a row
-  float win_ks[kUnit];                             // window rows: the largest of the key's scales
+  float win_ks[NH == 1 ? 1 : kUnit];                             // window rows: the largest of the key's scales
   float alpha[8];
 };
 
@@ -79,9 +79,11 @@ struct alignas(16) WaveMemory {
 // not have).
 template <int NH>
 struct alignas(16) Queries {
-  uint4 far[4][64], win[4][64];
+  uint4 far[4][64];
   uint4 third[NH == 8 ? 4 : 1][64];
+  uint4 win[NH == 1 ? 1 : 4][64];
   float win_scale[64];
+  float win_query[kD];   // one head
 };
 
 // The upper half of a float: bfloat16 by truncation, and what is left.
@@ -114,6 +116,17 @@ __device__ __forceinline__ void put_far_queries(const float* from, int i, bool a
 
 // The first of the eight elements of either half that a lane row has of a turned row; the next eight are 16 on.
 __device__ __forceinline__ int turned_from(int lrow) { return 32 * (lrow & 1) + 8 * (lrow >> 1); }
+
+// One head's window query times log2 e / sqrt(128).
+template <typename T>
+__device__ __forceinline__ void put_win_query(const T* from, int lane, float (&to)[kD]) {
+  if (lane < kD / 8) {
+    float x[8];
+    load8(from + lane * 8, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) to[lane * 8 + e] = x[e] * kLogit;
+  }
+}
 
 // Slice i of the window's queries (0, 1: eight elements of the lower half each, 2, 3: of the upper one), as float16 terms of x 2^(8 - e),
 // |x| < 2^e for all of the head: x = 2^(e - 8) (t0 + t1 + t2) but for 2^-33 of 2^e (half the least float16) and, for eight heads with their
@@ -153,12 +166,17 @@ __device__ __forceinline__ const uint8_t* row_byte(const uint8_t* rows, uint32_t
   if (PAGED) return rows + (size_t)r * kKv4RowBytes + at;
   return rows + (r * kKv4RowBytes + (uint32_t)at);
 }
-// A unit's keys or values as they come from memory (`at`: where in a row): 16 bytes of row `column` of each tile, by lane row.  Values by words
-// of the rows that a lane needs would be four times as many requests: 65 instead of 56 us for the rows of 32 x 28 heads.
+// A unit's keys and values as they come from memory: 16 bytes of either of row `column` of each tile, by lane row; a row's two requests, which are
+// for the same line, one after the other.  (Values by words of the rows that a lane needs would be four times as many requests: bare
+// loads of the rows of 32 x 28 heads take 65 us so, 56 like this, 54 by whole lines.)
 template <bool PAGED>
-__device__ __forceinline__ void load_rows(const uint8_t* cache, const uint32_t* rows, int at, int lane, i32x4 (&x)[4]) {
+__device__ __forceinline__ void load_rows(const uint8_t* cache, const uint32_t* rows, int lane, i32x4 (&k)[4], i32x4 (&v)[4]) {
 #pragma unroll
-  for (int t = 0; t < 4; ++t) x[t] = *(const i32x4*)row_byte<PAGED>(cache, rows[t * 16 + (lane & 15)], at + (lane >> 4) * 16);
+  for (int t = 0; t < 4; ++t) {
+    const uint8_t* p = row_byte<PAGED>(cache, rows[t * 16 + (lane & 15)], (lane >> 4) * 16);
+    k[t] = *(const i32x4*)p;
+    v[t] = *(const i32x4*)(p + kKv4Half);
+  }
 }
 
 // Products of the queries with a unit's far keys: row `column` of tile t in dot[t].
@@ -241,30 +259,76 @@ __device__ __forceinline__ f32x4 turned_dot(const i32x4& k, uint32_t sc, const f
   return acc;
 }
 
+// One head: products of the query with a tile's window keys, turned by the row's angles, on the vector ALU: of a pair of elements,
+//   (q R) . k = cos (q_l k_l + q_u k_u) + sin (q_l k_u - q_u k_l),
+// six operations, where the terms of turned keys are twelve.  Angles of eight pairs:
+struct Angles {
+  float cs[8], sn[8];
+  __device__ __forceinline__ void load(const float* cos_win, const float* sin_win, int delta, int lrow, int i) {
+    load8(cos_win + (size_t)delta * (kD / 2) + turned_from(lrow) + 16 * i, cs);
+    load8(sin_win + (size_t)delta * (kD / 2) + turned_from(lrow) + 16 * i, sn);
+  }
+};
+// ... pairs i of the lane row's two eights (see turned_dot): what the lane adds.
+__device__ __forceinline__ float turned_part(const i32x4& k, int i, float s_lower, float s_upper, const Angles& a, const float* query, int lrow) {
+  const auto words = __builtin_amdgcn_permlane32_swap((uint32_t)k[2 * i], (uint32_t)k[2 * i + 1], false, false);
+  float sum = 0.f;
+#define A2ATS_PAIR(e)                                                                          \
+  {                                                                                            \
+    const auto kl = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(words[0], s_lower, e);            \
+    const auto ku = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(words[1], s_upper, e);            \
+    _Pragma("unroll") for (int j = 0; j < 2; ++j) {                                            \
+      const int x = 2 * e + j;                                                                 \
+      sum += a.cs[x] * (ql[x % 4] * kl[j] + qu[x % 4] * ku[j]) + a.sn[x] * (ql[x % 4] * ku[j] - qu[x % 4] * kl[j]); \
+    }                                                                                          \
+  }
+#define A2ATS_FOUR(at, first, second)                                                          \
+  {                                                                                            \
+    int from = turned_from(lrow) + 16 * i + at;                                                \
+    asm volatile("" : "+v"(from));                                                             \
+    const f32x4 ql = *(const f32x4*)(query + from), qu = *(const f32x4*)(query + kD / 2 + from); \
+    A2ATS_PAIR(first) A2ATS_PAIR(second)                                                       \
+    __builtin_amdgcn_sched_barrier(0);                                                         \
+  }
+  // (The query is read again for each tile, four numbers of either half at a time: more would not fit the registers.)
+  A2ATS_FOUR(0, 0, 1)
+  A2ATS_FOUR(4, 2, 3)
+#undef A2ATS_FOUR
+#undef A2ATS_PAIR
+  return sum;
+}
+
 // The bits of a where the mask has ones, else those of b.
 __device__ __forceinline__ uint32_t select_bits(uint32_t mask, uint32_t a, uint32_t b) { return (mask & a) | (~mask & b); }
 
-// 32 rows' values, of which a lane has a word (two dimensions of each group) of the rows 4 e + lane row, e = 0 .. 7, so that what the lanes
-// of a wave read at a time is in one piece of LDS.  Two rows' words together: byte g of even[i] has the first of the two dimensions of group g
-// of the rows e = 2 i and 2 i + 1, of odd[i] the second; the lower half of a byte is the first row's.
+// Rows of a unit in LDS.  A lane has elements e = 0 .. 7 of either half h as operands of the second product: one head, rows 32 h + 4 e + lane
+// row; else rows 16 (e % 4) + 8 h + 2 lane row + e / 4, so that the four rows that a lane has weights of lie behind each other.  Values lie
+// so that what the lanes of a wave read at a time is in one piece.
+template <int NH>
+__device__ __forceinline__ int value_slot(int tile, int col) { return tile * 16 + (NH == 1 ? col : (col & 1) << 3 | col >> 1); }
+__device__ __forceinline__ int weight_at(int row) { return (row & 32) | (row & 3) << 3 | (row >> 2 & 7); }   // one head
+
+// A half's values, of which a lane has a word (two dimensions of each group) of its eight rows, two rows' words together: byte g of even[i]
+// has the first of the two dimensions of group g of the rows e = 2 i and 2 i + 1, of odd[i] the second; the lower half of a byte is the
+// first row's.
+template <int NH>
 struct Values {
   uint32_t even[4], odd[4];
-  __device__ __forceinline__ Values(const uint32_t* v) {   // word `column` of row `lane row`
+  __device__ __forceinline__ Values(const uint32_t* v, int h) {   // word `column` of slot `lane row`
+    auto word = [&](int e) { return v[(NH == 1 ? 32 * h + 4 * e : 16 * (e & 3) + 8 * (e >> 2) + 4 * h) * 16]; };
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t a = v[8 * i * 16], c = v[(8 * i + 4) * 16];
+      const uint32_t a = word(2 * i), c = word(2 * i + 1);
       even[i] = select_bits(0x0f0f0f0fu, a, c << 4);
       odd[i] = select_bits(0x0f0f0f0fu, a >> 4, c);
     }
   }
 };
-// Where a row's weight is among those of a column: row 32 h + 4 e + r is element e of lane row r, of half h.
-__device__ __forceinline__ int weight_at(int row) { return (row & 32) | (row & 3) << 3 | (row >> 2 & 7); }
 
 // Their products with the weights (columns of LDS; one head: a term a column, else three terms), added to the outputs: o[t][i] is
 // dimension 32 (t / 2) + 2 (4 * lane row + i) + t % 2, in the columns of group t / 2.  SET: eight heads, groups SET and 2 + SET.
 template <int NH, int SET>
-__device__ __forceinline__ void absorb(const Values& v, const uint16_t* weights, f32x4 (&o)[8]) {
+__device__ __forceinline__ void absorb(const Values<NH>& v, const uint16_t* weights, f32x4 (&o)[8]) {
   constexpr int kTerms = NH == 1 ? 1 : 3;
   bf16x8 b[kTerms];
 #pragma unroll
@@ -295,7 +359,7 @@ __device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
 
 // NH: heads that attend the same rows, one, or the G of a KV head if the selection is shared, padded to 4 or 8.
 template <typename T, int NH, bool PAGED>
-__global__ __launch_bounds__(kThreads, NH == 1 ? 4 : 2) void attn_kv4_kernel(Attn4Args a) {
+__global__ __launch_bounds__(kWaves * 64, NH == 1 ? 4 : 2) void attn_kv4_kernel(Attn4Args a) {
   typedef Layout<NH> L;
   __shared__ __align__(16) union {
     struct {
@@ -327,10 +391,10 @@ __global__ __launch_bounds__(kThreads, NH == 1 ? 4 : 2) void attn_kv4_kernel(Att
   const int n_sink = min(a.n_sink, a.ctx_len);
   const int win_tiles = (a.win_share + 16 * kWaves - 1) / (16 * kWaves), far_tiles = (a.far_share + 16 * kWaves - 1) / (16 * kWaves);
   const int f0 = part * a.far_share + (wv * far_tiles - win_tiles) * 16, w0 = part * a.win_share + wv * win_tiles * 16;
-  auto unit_of = [&](int u) {   // (clamped: requested before it is known to count)
+  auto unit_of = [&](int u, int lane) {   // (clamped: requested before it is known to count)
     return a.n_sel > 0 ? idx[min(max(f0 + u * kUnit + lane - n_sink, 0) >> a.sel_shift, a.n_sel - 1)] : 0;
   };
-  int index = unit_of(0);
+  int index = unit_of(0, lane);
   const SeqRange sr = seq_range(a.ctx_len, a.seq_lens, b, a.window, a.n_sink, 0);
   const int cnt = min(max(a.sel_count[sel], 0), a.n_sel);
   const int f1 = min(min((part + 1) * a.far_share, f0 + (win_tiles + far_tiles) * 16), n_sink + (cnt << a.sel_shift));
@@ -345,8 +409,8 @@ __global__ __launch_bounds__(kThreads, NH == 1 ? 4 : 2) void attn_kv4_kernel(Att
     uint2 sc;
     bool in;
   };
-  auto place = [&](uint32_t* to, int u) {
-    const int tile = 4 * u + lrow, t = f0 + u * kUnit + lane;
+  auto place = [&](uint32_t* to, int u, int lane) {
+    const int tile = 4 * u + (lane >> 4), t = f0 + u * kUnit + lane;
     bool in;
     int j = t;
     if (tile < win_tiles) {
@@ -381,16 +445,18 @@ __global__ __launch_bounds__(kThreads, NH == 1 ? 4 : 2) void attn_kv4_kernel(Att
   i32x4 k[4], v[4];
   Place at, next;
   if (units > 0) {
-    at = place(wm.row[0], 0);
-    load_rows<PAGED>(rows, wm.row[0], 0, lane, k);
-    load_rows<PAGED>(rows, wm.row[0], kKv4Half, lane, v);
-    index = unit_of(1);
+    at = place(wm.row[0], 0, lane);
+    load_rows<PAGED>(rows, wm.row[0], lane, k, v);
+    index = unit_of(1, lane);
   }
   {
     const size_t q_at = (size_t)(head + min(L::q_head(col), nh - 1)) * kD;
     const bool active = L::q_head(col) < nh;
     put_far_queries<NH>(a.q_rot + q_at + lrow * 32, wv, active, lane, s.in.queries);
-    if (a.window > 0) put_win_queries<T, NH>((const T*)a.q + q_at, wv, active, lane, s.in.queries);
+    if (a.window > 0) {
+      if constexpr (NH != 1) put_win_queries<T, NH>((const T*)a.q + q_at, wv, active, lane, s.in.queries);
+      else if (wv == 0) put_win_query((const T*)a.q + q_at, lane, s.in.queries.win_query);
+    }
   }
   if (NH == 1) wm.weights[NH == 1 ? 12 : 0][lane] = 0;
   __syncthreads();
@@ -401,10 +467,13 @@ __global__ __launch_bounds__(kThreads, NH == 1 ? 4 : 2) void attn_kv4_kernel(Att
   }
 #pragma unroll
   for (int t = 0; t < 8; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const uint16_t* my_weights = wm.weights[NH == 1 ? min(col, 12) : col] + lrow * 8;
 
 #pragma unroll 1
   for (int u = 0; u < units; ++u) {
+    int lane = tid & 63;
+    asm volatile("" : "+v"(lane));   // (else a dozen addresses are kept in registers, which there are not)
+    const int col = lane & 15, lrow = lane >> 4;
+    const uint16_t* my_weights = wm.weights[NH == 1 ? min(col, 12) : col] + lrow * 8;
     // The scales of this unit's rows, for the lanes that have them as keys, and the values, from where they are read again by rows.
     uint32_t most = 0;
 #pragma unroll
@@ -413,42 +482,63 @@ __global__ __launch_bounds__(kThreads, NH == 1 ? 4 : 2) void attn_kv4_kernel(Att
     wave_exchange();
     wm.ksc[lane] = at.sc.x;
     if (NH != 1) {
-      wm.vsc[NH == 1 ? 0 : lane] = at.sc.y;
+      wm.vsc[NH == 1 ? 0 : lane] = at.in ? at.sc.y : 0u;
       wm.ks[NH == 1 ? 0 : lane] = at.in ? ks : -1.f;
     }
-    if (4 * u < win_tiles) wm.win_ks[lane] = kv4_scale(most);
+    if (NH != 1 && 4 * u < win_tiles) wm.win_ks[NH == 1 ? 0 : lane] = kv4_scale(most);
 #pragma unroll
-    for (int t = 0; t < 4; ++t) wm.values[t * 16 + col][lrow] = v[t];
+    for (int t = 0; t < 4; ++t) wm.values[value_slot<NH>(t, col)][lrow] = v[t];
     wave_exchange();
     uint32_t* next_rows = wm.row[(u & 1) ^ 1];
-    next = place(next_rows, u + 1);
-    index = unit_of(u + 2);
+    next = place(next_rows, u + 1, lane);
+    index = unit_of(u + 2, lane);
 
     f32x4 dot[4];
     far_dots<NH>(k, (const uint8_t*)wm.ksc, lane, s.in.queries, dot);
-    if (4 * u < win_tiles) {
+    float lg[4];   // one head
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        if (4 * u + t < win_tiles) {
-          const int delta = min(max(sr.n - 1 - (sr.win_start + w0 + u * kUnit + t * 16 + col), 0), a.window - 1);
+    for (int t = 0; t < 4; ++t) lg[t] = dot[t][0] + dot[t][1] + dot[t][2];
+    if (4 * u < win_tiles) {
+      __builtin_amdgcn_sched_barrier(0);
+      auto distance = [&](int t) { return min(max(sr.n - 1 - (sr.win_start + w0 + u * kUnit + t * 16 + col), 0), a.window - 1); };
+      if constexpr (NH == 1) {   // (the angles of the next eight pairs are requested before these are used)
+        Angles x, y;
+        x.load(a.cos_win, a.sin_win, distance(0), lrow, 0);
+        const int tiles = min(win_tiles - 4 * u, 4);
+#pragma unroll 1
+        for (int t = 0; t < tiles; ++t) {
+          const i32x4 kt = t < 2 ? (t == 0 ? k[0] : k[1]) : (t == 2 ? k[2] : k[3]);
+          const uint32_t sc = wm.ksc[t * 16 + col];
+          const float s_lower = kv4_scale((sc >> (8 * (lrow & 1))) & 255u), s_upper = kv4_scale((sc >> (16 + 8 * (lrow & 1))) & 255u);
+          y.load(a.cos_win, a.sin_win, distance(t), lrow, 1);
+          float sum = turned_part(kt, 0, s_lower, s_upper, x, s.in.queries.win_query, lrow);
+          x.load(a.cos_win, a.sin_win, distance(t + 1), lrow, 0);
+          sum += turned_part(kt, 1, s_lower, s_upper, y, s.in.queries.win_query, lrow);
+          sum = rows_sum(sum);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) lg[i] = t == i ? sum : lg[i];
+        }
+        // The angles requested last are used by nobody: here, else all units wait for what is requested at this place.
+        __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+      } else {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          if (4 * u + t >= win_tiles) break;
+          const int delta = distance(t);
           dot[t] = turned_dot<NH>(k[t], wm.ksc[t * 16 + col], a.cos_win + (size_t)delta * (kD / 2), a.sin_win + (size_t)delta * (kD / 2), lane,
                                   s.in.queries);
           // (of the query's row 4 * lane row: the terms of a head have the same)
-          dot[t] *= wm.win_ks[t * 16 + col];
+          dot[t] *= wm.win_ks[NH == 1 ? 0 : t * 16 + col];
           const float4 qs = *(const float4*)(s.in.queries.win_scale + 4 * lrow);
           dot[t] = f32x4{dot[t][0] * qs.x, dot[t][1] * qs.y, dot[t][2] * qs.z, dot[t][3] * qs.w};
         }
       }
     }
-    load_rows<PAGED>(rows, next_rows, 0, lane, k);
-    load_rows<PAGED>(rows, next_rows, kKv4Half, lane, v);
+    load_rows<PAGED>(rows, next_rows, lane, k, v);
 
     // Logits: one head, of the lane's own row; else of row `column` of each tile, of the lane row's heads.
     float p[L::kOwn];
     if constexpr (NH == 1) {
-      float lg[4];
-#pragma unroll
-      for (int t = 0; t < 4; ++t) lg[t] = dot[t][0] + dot[t][1] + dot[t][2];
       const float x = (lrow & 2) ? ((lrow & 1) ? lg[3] : lg[2]) : ((lrow & 1) ? lg[1] : lg[0]);
       p[0] = at.in ? x * ks : -INFINITY;
     } else {
@@ -502,42 +592,51 @@ __global__ __launch_bounds__(kThreads, NH == 1 ? 4 : 2) void attn_kv4_kernel(Att
     }
 
     // Weights times the scales of the groups, as three bfloat16 terms, into the columns of the second product.
-    auto put = [&](float x, int c0, int step, int row) {
-#pragma unroll
-      for (int term = 0; term < 3; ++term) {
-        wm.weights[c0 + term * step][weight_at(row)] = upper_half(x);
-        x = lower_part(x);
-      }
-    };
     const uint32_t* words = (const uint32_t*)&wm.values[lrow][0] + col;
     if constexpr (NH == 1) {
       const uint32_t vsc = at.in ? at.sc.y : 0u;
 #pragma unroll
-      for (int g = 0; g < 4; ++g) put(p[0] * kv4_scale((vsc >> (8 * g)) & 255u), g, 4, lane);
+      for (int g = 0; g < 4; ++g) {
+        float x = p[0] * kv4_scale((vsc >> (8 * g)) & 255u);
+#pragma unroll
+        for (int term = 0; term < 3; ++term) {
+          wm.weights[4 * term + g][weight_at(lane)] = upper_half(x);
+          x = lower_part(x);
+        }
+      }
       wave_exchange();
-      absorb<NH, 0>(Values(words), my_weights, o);
-      absorb<NH, 0>(Values(words + kUnit / 2 * 16), my_weights + kUnit / 2, o);
+      absorb<NH, 0>(Values<NH>(words, 0), my_weights, o);
+      absorb<NH, 0>(Values<NH>(words, 1), my_weights + kUnit / 2, o);
     } else {
 #pragma unroll
       for (int set = 0; set < (NH == 8 ? 2 : 1); ++set) {
         wave_exchange();
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const uint32_t vsc = wm.ks[NH == 1 ? 0 : t * 16 + col] < 0.f ? 0u : wm.vsc[NH == 1 ? 0 : t * 16 + col];
+        for (int g = 0; g < (NH == 8 ? 2 : 4); ++g) {
+          float sc[4];
 #pragma unroll
-          for (int h = 0; h < L::kHeads; ++h)
+          for (int t = 0; t < 4; ++t) sc[t] = kv4_scale((wm.vsc[NH == 1 ? 0 : t * 16 + col] >> (8 * (NH == 8 ? 2 * g + set : g))) & 255u);
 #pragma unroll
-            for (int g = 0; g < (NH == 8 ? 2 : 4); ++g)
-              put(p[t * L::kHeads + h] * kv4_scale((vsc >> (8 * (NH == 8 ? 2 * g + set : g))) & 255u),
-                  NH == 8 ? 2 * (2 * lrow + h) + g : 4 * lrow + g, 16, t * 16 + col);
+          for (int h = 0; h < L::kHeads; ++h) {
+            float x[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) x[t] = p[t * L::kHeads + h] * sc[t];
+#pragma unroll
+            for (int term = 0; term < 3; ++term) {
+              *(uint2*)&wm.weights[16 * term + (NH == 8 ? 2 * (2 * lrow + h) + g : 4 * lrow + g)][4 * col] =
+                  make_uint2(upper_halves(x[0], x[1]), upper_halves(x[2], x[3]));
+#pragma unroll
+              for (int t = 0; t < 4; ++t) x[t] = lower_part(x[t]);
+            }
+          }
         }
         wave_exchange();
         if (set == 0) {
-          absorb<NH, 0>(Values(words), my_weights, o);
-          absorb<NH, 0>(Values(words + kUnit / 2 * 16), my_weights + kUnit / 2, o);
+          absorb<NH, 0>(Values<NH>(words, 0), my_weights, o);
+          absorb<NH, 0>(Values<NH>(words, 1), my_weights + kUnit / 2, o);
         } else {
-          absorb<NH, 1>(Values(words), my_weights, o);
-          absorb<NH, 1>(Values(words + kUnit / 2 * 16), my_weights + kUnit / 2, o);
+          absorb<NH, 1>(Values<NH>(words, 0), my_weights, o);
+          absorb<NH, 1>(Values<NH>(words, 1), my_weights + kUnit / 2, o);
         }
       }
     }
@@ -591,17 +690,41 @@ __global__ __launch_bounds__(kThreads, NH == 1 ? 4 : 2) void attn_kv4_kernel(Att
 
 }  // namespace
 
+// Parts: a second launch that joins them, 3 us, against units of 64 rows that a wave has to take one after the other, 1.5 us each (2.6 for
+// heads that share a selection) while there is a workgroup a CU at most.  So: the least parts that leave a wave the fewest units, with no more
+// workgroups than CUs, where that saves two units.  Measured for 2 to 896 problems of 160 to 4160 rows with 1 to 16 parts (bfloat16, window
+// 64), us with one part -> with the parts taken: 2 problems, 576 rows 10.1 -> 9.5 (3 parts), 2304 rows 18.1 -> 10.4 (12); 32 problems, 1152
+// rows 12.9 -> 10.0 (6), 4160 rows 28.5 -> 13.0 (6); 128 problems, 2304 rows 19.3 -> 17.1 (2; four: 18.5); 256 problems, 2304 rows would be
+// 20.2 -> 23.9; shared by four heads, 8 problems, 1152 rows 19.2 -> 12.4 (6), 128 problems, 1152 rows 20.4 -> 19.7 (2).  Many rows of problems
+// that leave half a round of CUs over: 896 problems, 4160 rows 102 -> 96 (2), 384 problems 48.1 -> 44.1, but with 2304 rows 61.7 -> 62.1.
 Kv4Plan make_kv4_plan(const a2ats_dims& d, long sel_rows, int window, bool shared) {
-  Kv4Plan p;
   const long problems = (long)d.batch * (shared ? d.n_kv_heads : d.n_q_heads);
-  const long rows = std::min<long>(sel_rows, d.ctx_len) + std::min(window, d.ctx_len);
+  const long far = std::min<long>(sel_rows, d.ctx_len), win = std::min(window, d.ctx_len);
+  auto units = [&](long parts) {
+    const long f = (far + parts - 1) / parts, w = (win + parts - 1) / parts;
+    return ((f + 16 * kWaves - 1) / (16 * kWaves) + (w + 16 * kWaves - 1) / (16 * kWaves) + 3) / 4;
+  };
   long parts = 1;
-  if (problems <= 64) parts = rows < 350 ? 1 : std::min(std::min(problems > 0 ? 256 / problems : 1, rows / 72), 12l);
-  else if (problems <= 128) parts = rows >= 1600 ? 4 : (rows >= 800 ? 2 : 1);
-  else if (problems < 512) parts = rows >= 1600 ? 2 : 1;
+  for (long p = 2; p <= 12 && p * problems <= 256; ++p)
+    if (units(p) < units(parts)) parts = p;
+  if (units(1) - units(parts) < 2) parts = 1;
+  if (problems > 256 && problems % 256 == 128 && units(1) >= 16) parts = 2;
+  Kv4Plan p;
   p.parts = (int)parts;
   p.bytes = parts > 1 ? (size_t)d.batch * d.n_q_heads * parts * (kD + 2) * sizeof(float) : 0;
   return p;
+}
+
+// What every call with at most so many selected tokens and such a window needs.
+size_t kv4_ws_bytes(const a2ats_dims& d, long sel_rows, int window) {
+  const long rows = std::min<long>(sel_rows, d.ctx_len) + std::min(window, d.ctx_len);
+  size_t need = 0;
+  for (int shared = 0; shared < 2; ++shared) {
+    const long problems = (long)d.batch * (shared ? d.n_kv_heads : d.n_q_heads);
+    const long parts = problems <= 128 ? std::min(problems > 0 ? 256 / problems : 1, 12l) : (problems > 256 && problems % 256 == 128 ? 2 : 1);
+    if (parts > 1 && rows > 4 * kUnit) need = std::max(need, (size_t)d.batch * d.n_q_heads * parts * (kD + 2) * sizeof(float));
+  }
+  return need;
 }
 
 template <typename T, bool PAGED>
