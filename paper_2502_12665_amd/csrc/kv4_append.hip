@@ -23,25 +23,169 @@ __device__ __forceinline__ uint32_t lane_of(uint32_t v) {
 constexpr int kXor1 = 0xB1, kXor2 = 0x4E;              // quad_perm [1,0,3,2], [2,3,0,1]
 constexpr int kNext4 = 0x12C, kNext8 = 0x128, kNext12 = 0x124;   // row_ror: of 16 lanes, the one 4, 8, 12 further on
 
-// Eight elements of a row, of which 16 consecutive lanes have all, as codes, the first in the lowest bits; the scale byte of the
-// group, which four lanes share.
-__device__ __forceinline__ uint32_t codes8(const float (&x)[8], uint32_t& byte) {
-  uint32_t big = 0;
+typedef __attribute__((ext_vector_type(2))) short i16x2;
+typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+
+// Eight elements of a row, of which 16 consecutive lanes have all, as they come from memory.
+template <typename T>
+struct Eight;
+template <>
+struct Eight<float> {
+  float x[8];
+  __device__ __forceinline__ void load(const float* p) { load8(p, x); }
+  __device__ __forceinline__ void zero() {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) big = max(big, __float_as_uint(x[e]) & 0x7fffffffu);
+    for (int e = 0; e < 8; ++e) x[e] = 0.f;
+  }
+  __device__ __forceinline__ uint32_t largest() const {   // magnitude, as bits
+    uint32_t big = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) big = max(big, __float_as_uint(x[e]) & 0x7fffffffu);
+    return big;
+  }
+  __device__ __forceinline__ uint32_t codes(float scale) const {   // the first in the lowest bits
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], scale, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
+    return w;
+  }
+};
+template <>
+struct Eight<uint16_t> {
+  uint32_t x[4];
+  __device__ __forceinline__ void load(const uint16_t* p) {
+    const uint4 v = *(const uint4*)p;
+    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+  }
+  __device__ __forceinline__ void zero() { x[0] = x[1] = x[2] = x[3] = 0u; }
+  __device__ __forceinline__ uint32_t largest() const {   // (two at a time, 16 bits each)
+    u16x2 big = __builtin_bit_cast(u16x2, x[0] & 0x7fff7fffu);
+#pragma unroll
+    for (int e = 1; e < 4; ++e) big = __builtin_elementwise_max(big, __builtin_bit_cast(u16x2, x[e] & 0x7fff7fffu));
+    return (uint32_t)max(big[0], big[1]) << 16;
+  }
+  __device__ __forceinline__ uint32_t codes(float scale) const {
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x[0]), scale, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x[1]), scale, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x[2]), scale, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x[3]), scale, 3);
+    return w;
+  }
+};
+
+// Their codes, and the scale byte of the group, which four lanes share.
+template <typename T>
+__device__ __forceinline__ uint32_t codes8(const Eight<T>& x, uint32_t& byte) {
+  uint32_t big = x.largest();
   big = max(big, lane_of<kXor1>(big));
   big = max(big, lane_of<kXor2>(big));
   const bool usable = big >= kTinyBits && big < kHugeBits;
   // 6 = 1.5 * 2^2
   byte = usable ? (big >> 23) - 2u + ((big & 0x7fffffu) > 0x400000u ? 1u : 0u) : (big < kTinyBits ? 0u : 255u);
-  const float scale = kv4_scale(usable ? byte : 127u);
-  uint32_t w = 0;
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], scale, 0);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
+  const uint32_t w = x.codes(kv4_scale(usable ? byte : 127u));
   return usable ? w : 0u;
 }
+
+// The smallest and largest key of each of eight dimensions: of a lane's rows, then of the lane rows, whose bounds of two dimensions lane row r
+// is left with (2 r and 2 r + 1), then of the waves (from LDS).
+template <typename T>
+struct Bounds;
+template <>
+struct Bounds<float> {
+  typedef float Elem;
+  float lo[8], hi[8];
+  bool any_nan;
+  __device__ __forceinline__ Bounds() : any_nan(false) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { lo[e] = INFINITY; hi[e] = -INFINITY; }
+  }
+  // `there`: the row counts.
+  __device__ __forceinline__ void add(const Eight<float> (&x)[4], const bool (&there)[4]) {
+    uint32_t big = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) big = max(big, x[i].largest());
+    any_nan = __builtin_amdgcn_ballot_w64(big > 0x7f800000u) != 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (there[i]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          lo[e] = any_nan ? low(lo[e], x[i].x[e]) : min2(lo[e], x[i].x[e]);
+          hi[e] = any_nan ? high(hi[e], x[i].x[e]) : max2(hi[e], x[i].x[e]);
+        }
+      }
+  }
+  __device__ __forceinline__ void store(float* s_lo, float* s_hi) const {
+    *(float2*)s_lo = any_nan ? over_lane_rows(lo, low) : over_lane_rows(lo, min2);
+    *(float2*)s_hi = any_nan ? over_lane_rows(hi, high) : over_lane_rows(hi, max2);
+  }
+  static __device__ __forceinline__ float none_low() { return INFINITY; }
+  static __device__ __forceinline__ float none_high() { return -INFINITY; }
+  static __device__ __forceinline__ float of(float x) { return x; }
+  static __device__ __forceinline__ float least(float a, float b) { return low(a, b); }
+  static __device__ __forceinline__ float most(float a, float b) { return high(a, b); }
+  static __device__ __forceinline__ void put(float* p, float lo, float hi) {
+    p[0] = lo;
+    p[D] = hi;
+  }
+};
+// bfloat16, two at a time, as whole numbers of the same order: the lower 15 bits of negative ones turned over.  What is not a number is beyond
+// the infinities, by its sign, and makes both bounds one at the end.
+template <>
+struct Bounds<uint16_t> {
+  typedef short Elem;
+  i16x2 lo[4], hi[4];
+  __device__ __forceinline__ Bounds() {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { lo[e] = i16x2{0x7fff, 0x7fff}; hi[e] = i16x2{-0x8000, -0x8000}; }
+  }
+  __device__ __forceinline__ void add(const Eight<uint16_t> (&x)[4], const bool (&there)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (there[i]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const i16x2 y = __builtin_bit_cast(i16x2, x[i].x[e]);
+          const i16x2 z = y ^ ((y >> 15) & i16x2{0x7fff, 0x7fff});
+          lo[e] = __builtin_elementwise_min(lo[e], z);
+          hi[e] = __builtin_elementwise_max(hi[e], z);
+        }
+      }
+  }
+  template <typename F>
+  static __device__ __forceinline__ uint32_t pair(uint32_t a, uint32_t b, F f) {
+    return __builtin_bit_cast(uint32_t, f(__builtin_bit_cast(i16x2, a), __builtin_bit_cast(i16x2, b)));
+  }
+  template <typename F>
+  static __device__ __forceinline__ uint32_t over_rows(const i16x2 (&v)[4], F f) {
+    uint32_t h[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const auto s = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v[e]), __builtin_bit_cast(uint32_t, v[e + 2]), false, false);
+      h[e] = pair(s[0], s[1], f);
+    }
+    const auto s = __builtin_amdgcn_permlane16_swap(h[0], h[1], false, false);
+    return pair(s[0], s[1], f);
+  }
+  __device__ __forceinline__ void store(short* s_lo, short* s_hi) const {
+    *(uint32_t*)s_lo = over_rows(lo, [](i16x2 a, i16x2 b) { return __builtin_elementwise_min(a, b); });
+    *(uint32_t*)s_hi = over_rows(hi, [](i16x2 a, i16x2 b) { return __builtin_elementwise_max(a, b); });
+  }
+  static __device__ __forceinline__ short none_low() { return 0x7fff; }
+  static __device__ __forceinline__ short none_high() { return -0x8000; }
+  static __device__ __forceinline__ short of(uint16_t x) { return (short)(x ^ (((short)x >> 15) & 0x7fff)); }
+  static __device__ __forceinline__ short least(short a, short b) { return b < a ? b : a; }
+  static __device__ __forceinline__ short most(short a, short b) { return b > a ? b : a; }
+  static __device__ __forceinline__ void put(uint16_t* p, short lo, short hi) {
+    const bool nan = hi > 0x7f80 || lo < -0x7f81;
+    p[0] = nan ? (uint16_t)0x7fc0 : (uint16_t)of((uint16_t)lo);
+    p[D] = nan ? (uint16_t)0x7fc0 : (uint16_t)of((uint16_t)hi);
+  }
+};
 
 // A value's bytes in the order of the cache.  Lane j = 4 g + h of 16 has the dimensions 32 g + 8 h + 0 .. 7, bytes n = 4 h + 0 .. 3 of
 // group g; it is left with the word of n = 4 h + g, byte i of group i.
@@ -64,7 +208,8 @@ __global__ __launch_bounds__(NW * 64) void kv4_append_kernel(Kv4Cache m, const T
                                                              int n_new, int ctx_len, const int32_t* __restrict__ seq_lens,
                                                              const int32_t* __restrict__ new_lens, int parts) {
   constexpr int NT = NW * 64, SLAB = NW * kWaveRows;
-  __shared__ __align__(8) float s_lo[NW][D], s_hi[NW][D];
+  typedef typename Bounds<T>::Elem Bound;
+  __shared__ __align__(8) Bound s_lo[NW][D], s_hi[NW][D];
   // workgroups: [b][kv][part][key, value]
   const int what = blockIdx.x & 1, rest = blockIdx.x >> 1, part = rest % parts, bh = rest / parts;
   const int b = bh / m.at.n_kv_heads, kv = bh % m.at.n_kv_heads;
@@ -83,13 +228,14 @@ __global__ __launch_bounds__(NW * 64) void kv4_append_kernel(Kv4Cache m, const T
   const int w0 = r0 + wv * kWaveRows;                                  // the wave's rows lie in one block
   const bool live = w0 < n && w0 + kWaveRows > start;                  // some of them are new
 
-  float x[4][8];
+  Eight<T> x[4];
+  bool there[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int row = w0 + i * 4 + slot;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
-    if (row >= start && row < n) load8(fresh + (size_t)(row - start) * D + d0, x[i]);
+    there[i] = row >= start && row < n;
+    x[i].zero();
+    if (there[i]) x[i].load(fresh + (size_t)(row - start) * D + d0);
   }
   if (live) {
     const size_t at = (block_at(m.at, b, kv, w0 >> shift) << shift) + (size_t)(w0 & (blk - 1));
@@ -97,14 +243,13 @@ __global__ __launch_bounds__(NW * 64) void kv4_append_kernel(Kv4Cache m, const T
     const int word = what ? 16 + 4 * (j & 3) + (j >> 2) : j;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int row = w0 + i * 4 + slot;
       uint32_t byte;
       uint32_t w = codes8(x[i], byte);
       if (what) w = order.apply(w);
       byte <<= 8 * (j >> 2);
       byte |= lane_of<kNext4>(byte);
       byte |= lane_of<kNext8>(byte);
-      if (row >= start && row < n) {
+      if (there[i]) {
         const size_t r = at + (size_t)(i * 4 + slot);
         *(uint32_t*)(m.rows + r * kKv4RowBytes + word * 4) = w;
         if (j == 0) *(uint32_t*)(m.scales + r * kKv4ScaleBytes + what * 4) = byte;
@@ -112,47 +257,26 @@ __global__ __launch_bounds__(NW * 64) void kv4_append_kernel(Kv4Cache m, const T
     }
   }
   if (!bounds) return;   // (uniform)
-  uint32_t big = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) big = max(big, __float_as_uint(x[i][e]) & 0x7fffffffu);
-  const bool any_nan = __builtin_amdgcn_ballot_w64(big > 0x7f800000u) != 0u;
-  float lo[8], hi[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) { lo[e] = INFINITY; hi[e] = -INFINITY; }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = w0 + i * 4 + slot;
-    if (row >= start && row < n) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        lo[e] = any_nan ? low(lo[e], x[i][e]) : min2(lo[e], x[i][e]);
-        hi[e] = any_nan ? high(hi[e], x[i][e]) : max2(hi[e], x[i][e]);
-      }
-    }
-  }
-  const int d2 = d0 + 4 * (slot >> 1) + 2 * (slot & 1);
-  *(float2*)&s_lo[wv][d2] = any_nan ? over_lane_rows(lo, low) : over_lane_rows(lo, min2);
-  *(float2*)&s_hi[wv][d2] = any_nan ? over_lane_rows(hi, high) : over_lane_rows(hi, max2);
+  Bounds<T> bd;
+  bd.add(x, there);
+  bd.store(&s_lo[wv][d0 + 2 * slot], &s_hi[wv][d0 + 2 * slot]);
   __syncthreads();
   const int per = blk / kWaveRows;   // waves of a block
   T* all = (T*)m.at.bounds;
   for (int i = tid; i < SLAB / blk * D; i += NT) {
     const int cb = i / D, d = i % D, ci = (r0 >> shift) + cb, t0 = ci << shift;
     if (t0 >= n) break;
-    float lo1 = INFINITY, hi1 = -INFINITY;
+    Bound lo = Bounds<T>::none_low(), hi = Bounds<T>::none_high();
     for (int w = cb * per; w < (cb + 1) * per; ++w) {
-      lo1 = low(lo1, s_lo[w][d]);
-      hi1 = high(hi1, s_hi[w][d]);
+      lo = Bounds<T>::least(lo, s_lo[w][d]);
+      hi = Bounds<T>::most(hi, s_hi[w][d]);
     }
     T* p = all + block_at(m.at, b, kv, ci) * 2 * D + d;
     if (t0 < start) {   // the block had tokens before
-      lo1 = low(lo1, get_elem(p));
-      hi1 = high(hi1, get_elem(p + D));
+      lo = Bounds<T>::least(lo, Bounds<T>::of(p[0]));
+      hi = Bounds<T>::most(hi, Bounds<T>::of(p[D]));
     }
-    put_elem(p, lo1);
-    put_elem(p + D, hi1);
+    Bounds<T>::put(p, lo, hi);
   }
 }
 
