@@ -541,8 +541,8 @@ def group_shared_step(args, torch, B, synth, wl):
 
 
 class BlockCacheSteps:
-    """Decode steps of a sequence (batch) over a cache in 8 bits cut into blocks of 16 tokens: all blocks but the last of the workload's
-    ctx_len tokens are appended before, and step i appends token i % tokens of the last one, selects as many blocks as hold top_k
+    """Decode steps of a sequence (batch) over a cache in 8 bits (codes "e2m1": in 4) cut into blocks of 16 tokens: all blocks but the
+    last of the workload's ctx_len tokens are appended before, and step i appends token i % tokens of the last one, selects as many blocks as hold top_k
     tokens, and attends them and the window.  So the incomplete block has one token, two, .. as in generation, the last step
     completes it, and the step behind that begins the block again."""
 
@@ -552,15 +552,18 @@ class BlockCacheSteps:
         self.tokens = N - self.first
         x = synth.make_decode_inputs(wl, device=device)
         self.dims = B.make_dims(wl.batch, wl.n_q_heads, wl.n_kv_heads, wl.head_dim, wl.n_sub, N, self.first + blk)
-        self.cache = B.KvBlocks.empty(self.dims, blk, x["q"].dtype, codes, device=device)
+        four = codes == "e2m1"
+        self.cache = B.Kv4Cache.empty(self.dims, blk, x["q"].dtype, device=device) if four else \
+            B.KvBlocks.empty(self.dims, blk, x["q"].dtype, codes, device=device)
         self.state = B.BlockDecodeState(self.dims, self.cache, -(-wl.top_k // blk), wl.window, wl.n_sink, x["inv_freq"], wl.wrope_b, shared,
                                         scores=False)
         self.q, at = x["q"], self.first
         self.lens = [torch.full((wl.batch,), at + t + 1, dtype=torch.int32, device=device) for t in range(self.tokens)]
         self.new = [tuple(x[c][:, :, at + t:at + t + 1].contiguous() for c in ("k", "v")) for t in range(self.tokens)]
         if at > 0:
-            B.kv8_append(self.dims, self.cache, x["k"][:, :, :at].contiguous(), x["v"][:, :, :at].contiguous(), at,
-                         torch.full((wl.batch,), at, dtype=torch.int32, device=device))
+            append = B.kv4_append if four else B.kv8_append
+            append(self.dims, self.cache, x["k"][:, :, :at].contiguous(), x["v"][:, :, :at].contiguous(), at,
+                   torch.full((wl.batch,), at, dtype=torch.int32, device=device))
 
     def step(self, i):
         t = i % self.tokens
@@ -568,12 +571,13 @@ class BlockCacheSteps:
 
 
 def block_cache_step(args, torch, B, synth, wl):
-    """A decode step over a cache in 8 bits cut into blocks of 16 tokens (no codebook): a2ats_kv8_append of the current token,
-    a2ats_block_topk of as many blocks as hold the workload's top_k tokens, a2ats_sparse_attn_kv8 over them and the window;
-    with --group-shared one selection per KV head.  The steps go through the last block's tokens, so the average is over
+    """A decode step over a cache in 8 or 4 bits cut into blocks of 16 tokens (no codebook): a2ats_kv8_append (a2ats_kv4_append) of the
+    current token, a2ats_block_topk of as many blocks as hold the workload's top_k tokens, a2ats_sparse_attn_kv8 (.._kv4) over them and
+    the window; with --group-shared one selection per KV head.  The steps go through the last block's tokens, so the average is over
     all fills of the incomplete block."""
     N, K, w = wl.ctx_len, wl.top_k, wl.window
-    codes = torch.int8 if args.block_cache == "i8" else torch.float8_e4m3fn
+    codes = {"i8": torch.int8, "e4m3": torch.float8_e4m3fn, "e2m1": "e2m1"}[args.block_cache]
+    bits = 4 if args.block_cache == "e2m1" else 8
     R = max(1, args.replicas)
     reps = [BlockCacheSteps(torch, B, synth, wl.replace(seed=wl.seed + r), codes, args.group_shared) for r in range(R)]
     blk, tokens = reps[0].block, reps[0].tokens
@@ -609,10 +613,10 @@ def block_cache_step(args, torch, B, synth, wl):
     heads = wl.n_kv_heads if args.group_shared else wl.n_q_heads
     mean = reps[0].first + (tokens + 1) / 2
     bounds_bytes = wl.batch * wl.n_kv_heads * ((N - w) // blk) * 2 * wl.head_dim * reps[0].q.element_size()
-    attn_bytes = wl.batch * heads * (K + w) * 2 * wl.head_dim
+    attn_bytes = wl.batch * heads * (K + w) * (2 * wl.head_dim if bits == 8 else wl.head_dim + 8)
     print(json.dumps({
-        "metric": "cached keys/s = B * Hkv * tokens / time of a WHOLE decode step over an 8-bit cache (append 1 token + block selection + "
-                  "sparse attention)",
+        "metric": f"cached keys/s = B * Hkv * tokens / time of a WHOLE decode step over a cache in {bits} bits (append 1 token + block "
+                  "selection + sparse attention)",
         "value": wl.batch * wl.n_kv_heads * mean / (ms * 1e-3), "unit": "keys/s", "n_gpus": 1, "steps": args.steps,
         "warmup": args.warmup, "ms_per_step": ms, "launch": launch, "ms_per_step_eager": ms_eager, "higher_is_better": True,
         "scaling": "weak", "vs_baseline": None, "dtype": f"{args.block_cache} K/V, f32 accumulate; {wl.kv_dtype} bounds, f64 decisions",
@@ -737,8 +741,8 @@ def main():
     ap.add_argument("--paged-codes", type=int, default=0,
                     help="time the score/top-K phase over a code matrix in pages of this many tokens beside the "
                          "contiguous one; prints a line of its own")
-    ap.add_argument("--block-cache", choices=["i8", "e4m3"],
-                    help="decode steps over a cache in 8 bits cut into blocks, which bounds of the keys select (with "
+    ap.add_argument("--block-cache", choices=["i8", "e4m3", "e2m1"],
+                    help="decode steps over a cache in 8 (or 4) bits cut into blocks, which bounds of the keys select (with "
                          "--group-shared: one selection per KV head); prints a line of its own.  In a graph where --steps is a "
                          "multiple of 16 * --replicas (each cache goes through the 16 fills of its last block)")
     ap.add_argument("--encode-prefill", action="store_true",

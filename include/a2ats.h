@@ -542,8 +542,9 @@ typedef struct a2ats_kv4 {
  * afterwards, the last m_b of them are rows 0 .. m_b - 1 of k_new / v_new.  Which tokens come in which call does not matter, and
  * tokens may be written again (with bounds: from the beginning of a block on; otherwise they stay bounds of what was there too).
  * With a = max |x| over a group: scale 2^e, the least power of two with a <= 6 * 2^e; codes x / 2^e rounded to the nearest
- * e2m1 number, ties to even, as for real numbers, with the sign of x.  a < 2^-100: scale byte 0 and codes 0.  A group with an element that is not finite, or a >=
- * 2^127: scale NaN and codes 0, so that what attends it is NaN (of a value: in that group's dimensions).
+ * e2m1 number, ties to even, as for real numbers, with the sign of x.  a < 2^-100: scale byte 0 and codes 0.  A group with an
+ * element that is not finite, or a >= 2^127: scale NaN and codes 0, so that what attends it is NaN (of a value: in that group's
+ * dimensions).
  * bounds (if not NULL) are those of the keys as given, as in a2ats_kv8_append.  Nothing else is written.  n_new == 0 is a no-op.
  */
 int a2ats_kv4_append(const a2ats_dims* dims, const a2ats_kv4* cache, const void* k_new, const void* v_new, int32_t n_new,
@@ -561,9 +562,10 @@ int a2ats_kv4_read(const a2ats_dims* dims, const a2ats_kv4* cache, int32_t n_row
 
 /*
  * a2ats_sparse_attn_kv8 over a cache in 4 bits: arguments, attended set and results as there, every row code * scale.  Products,
- * sums and weights are those of float32 (queries, weights and far keys enter their products whole; turned window keys as two float16 numbers, off by at
- * most 2^-23 of each element and 2^-26 of the row's largest, and for 5 to 8 heads of a shared selection the queries of window rows likewise).  The block selection over such a cache is
- * a2ats_block_topk, given its bounds, block, kv_dtype, page_table and page_size in an a2ats_kv_blocks.
+ * sums and weights are those of float32 (queries, weights and keys enter their products whole; but for two heads or more of a shared
+ * selection the turned keys of window rows are two float16 numbers, off by at most 2^-23 of each element and 2^-26 of the row's
+ * largest, and for 5 to 8 heads the queries of window rows are too).  The block selection over such a cache is a2ats_block_topk,
+ * given its bounds, block, kv_dtype, page_table and page_size in an a2ats_kv_blocks.
  * Workspace: a2ats_workspace_bytes(dims, A2ATS_OP_ATTN_KV4, n_sel * sel_size, window).
  */
 int a2ats_sparse_attn_kv4(const a2ats_dims* dims, const a2ats_kv4* cache, const void* q, const float* q_rot, const int32_t* sel_idx,
@@ -587,7 +589,8 @@ int a2ats_sparse_attn_kv4(const a2ats_dims* dims, const a2ats_kv4* cache, const 
  *                                               attention) and keys to be cached (a2ats_kv4_append, a2ats_kv8_append) are not rotated
  *   q_pos, k_pos       [dev, out, nullable, dtype B*H*n_new*D]   y R_p: for the prompt's own attention
  * At least one output; outputs do not overlap inputs or each other.  Float32 arithmetic, each output rounded once; no square
- * overflows.  A row with an element that is not finite is not finite either: NaN where that element is infinite (or in all of the row, for a NaN).
+ * overflows.  A row with an element that is not finite is not finite either: NaN where that element is infinite (or in all of the
+ * row, for a NaN).
  * All pointers 16-byte aligned but for the lengths (4).  n_new == 0 is a no-op, n_new <= ctx_len.  No workspace.
  */
 int a2ats_qk_norm_rope(const a2ats_dims* dims, const void* q, int64_t q_stride, const void* k, int64_t k_stride, int dtype,

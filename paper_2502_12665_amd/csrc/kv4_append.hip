@@ -5,7 +5,12 @@
 // row depends on nothing but itself: there is no tail, and a token can be written again.  x / 2^e is exact, and
 // v_cvt_scalef32_pk_fp4_f32 rounds it as for real numbers.
 //
-// Both are streams, 2 * 128 * e bytes against 136.
+// Both are streams, 2 * 128 * e bytes against 136.  16 lanes have a row, eight elements each: a group's largest is two steps over
+// four lanes, and a wave stores whole rows of 64 bytes.  Keys and values have workgroups of their own (kv8_append.hip has them so, by which
+// a token of 16 sequences is twice as many workgroups).  Measured: append of 32768 tokens of 8 heads in bfloat16 43.8 us with bounds (170 MB,
+// 3.9 TB/s), 4 x 4 heads of 4099 tokens in float32 14.8 us (76 MB, 5.2 TB/s); a token of 16 x 8 heads 4.0 us, a launch.  bfloat16 is
+// rounded as it comes from memory, and its bounds are taken two at a time as whole numbers: as float32 it was 51.5 us.  Reading back 65536
+// tokens of 4 heads in bfloat16 35 us (170 MB, 4.9 TB/s), 4 x 4 heads of 4099 tokens in float32 14.5 us (5.2 TB/s).
 #include "internal.hpp"
 #include "kv_bounds.hpp"
 

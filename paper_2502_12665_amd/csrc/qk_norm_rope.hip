@@ -4,7 +4,9 @@
 // so that eps 2^-2e does not either.
 //
 // A stream: 128 e bytes a head in, as many for each output.  16 lanes a row, a wave four rows at a time of one token, so that
-// the token's angles are loaded once for 16 heads; the other half of a rotated pair is eight lanes on.
+// the token's angles are loaded once for 16 heads; the other half of a rotated pair is eight lanes on.  Measured: 32768 tokens of 32 + 8 heads in
+// bfloat16 with q_pos, k_norm and k_pos 163 us (755 MB, 4.6 TB/s); 4 x 1021 tokens of 28 + 4 heads in float32 20 us (87 MB, in
+// part from the caches); a token of 16 sequences 3.9 us, a launch.
 #include "internal.hpp"
 #include "kv_blocks.hpp"
 

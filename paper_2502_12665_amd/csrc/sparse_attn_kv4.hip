@@ -2,23 +2,34 @@
 // each 32 dimensions of a token's key and value:
 //     logit_j = (q~ . k_j) / sqrt(128)  (window rows: q R_delta for q~),  out = sum softmax(logit)_j v_j.
 //
-// A row is 128 bytes of codes and 8 of scales, 4 flop per byte and head: a gather.  Both products are on the matrix cores, also
-// for one head, with the 16 columns of a tile used for the precision of the float32 operand:
-//   - keys (A, 16 rows x 128) times queries (B).  Lane row r has the dimensions 32 r .. 32 r + 31 of its column's row, which is a group:
-//     16 bytes of codes and one scale, with which they become bfloat16 (exact: two bits of significand) as they are converted.  The
-//     query is three bfloat16 terms by truncation, all of its 24 bits, a column each (eight heads have two columns each, and a
-//     second product for the third term).  The products of 4-bit and 8-bit operands with scales of their own would take the codes as
-//     they are, but their sums are not those of float32 (off by up to 2^-13 of the sum of magnitudes, measured).
-//   - values (A, 16 dimensions x 32 rows) times weights (B).  Logits leave the first product with a head in each column and
-//     four rows of each of two tiles in each lane, which is the B operand of the second as it stands.  A row has four scales, which
-//     multiply the weight: a column takes the scale of one group, and of a tile's products only the columns of its own group count.
-//     One head: 16 columns are four groups times the three bfloat16 terms of a weight; up to four heads: head times group, and a
-//     product for each term; eight: head times half the groups, and two sets of weights.  A lane loads four bytes of each of its 8 rows,
-//     two dimensions of each group; two rows' words are put together by halves of bytes, and each byte is then a pair of
-//     rows of one dimension, which converts to two bfloat16.
-// Window rows are turned back by their distance, (q R_delta) . k = q . (k R_-delta), relative to the row's largest scale, and go
-// in as two float16 terms (2^-23 of an element, 2^-26 of the row's largest).
+// A row is 128 bytes of codes and 8 of scales, 4 flop per byte and head: a gather, of whole lines of memory.  Both products are on the
+// matrix cores, also for one head, with the 16 rows or columns of a tile used for the precision of the float32 operand:
+//   - queries (A, 16 rows) times keys (B, 16 rows of the cache).  A lane has 32 dimensions of a key, which are a group: 16 bytes of codes
+//     and one scale, with which they become bfloat16 (exact: two bits of significand) as they are converted.  The query is three
+//     bfloat16 terms by truncation, all of its 24 bits, each a row of the tile (eight heads have two rows each, and a second product for the
+//     third term); its rows are ordered so that a lane has all terms of its heads' logits of one key.  With one head a lane has
+//     one logit: with the keys as the first operand it had 16, and the softmax of 32 x 28 heads of 2176 rows took 4 us more.
+//     The products of 4-bit and 8-bit operands with scales of their own would take the codes as they are, but their sums are not those of
+//     float32 (off by up to 2^-13 of the sum of magnitudes, measured).
+//   - values (A, 16 dimensions x 32 rows) times weights (B).  A row has four scales, which multiply the weight: a column takes the scale of
+//     one group, and of a tile's products only the columns of its own group count.  One head: 16 columns are four groups times
+//     the three bfloat16 terms of a weight; up to four heads: head times group, and a product for each term; eight: head times
+//     half the groups, and two sets of weights.  Weights go to their columns through LDS.  So do the values, which come from memory 16
+//     bytes a lane; a lane then takes four bytes of each of its 8 rows, two dimensions of each group.  Two rows' words are put
+//     together by halves of bytes, and each byte is then a pair of rows of one dimension, which converts to two bfloat16.
+// Window rows are turned back by their distance, (q R_delta) . k = q . (k R_-delta): one head on the vector ALU, in float32; heads that share
+// a selection by products of queries with turned keys, relative to the row's largest scale, that go in as two float16 terms (2^-23 of an
+// element, 2^-26 of the row's largest).  (For one head those products took as long with a window, 71.1 against 71.9 us, and 62.5 against
+// 60.1 without one, by their registers.)
 // The statistics, all sums and the output are float32.  Logits are kept times log2 e, so that a weight is one exponential.
+//
+// What bounds it: the gather.  Bare loads of the 1.95 million rows of 32 x 28 heads that attend 2176 rows each take 54 us by whole lines (4.9
+// TB/s of the 265 MB that they are); this kernel 60 us without a window and 72 us with 128 rows of window, whose angles, 64 KB for a
+// head, pass through the first-level cache.  A row's key and value are requested one after the other, as they are one line: by
+// tiles of keys and then tiles of values it took 67 us.  With few heads it is the latency of a unit (64 rows a wave, of which the next is
+// in flight): 4 x 32 heads of 2304 rows 16.5 us and 3 us to join their parts, 7.6 us at the rate of a copy.  Workgroups of 8 and 16 waves
+// instead of 4 take as long or longer at nearly all sizes (128 problems, 2304 rows 18.5 and 20.7 us against 19.4; 896 problems 60.8 with
+// four), two units in flight for each wave too.
 #include <algorithm>
 
 #include "internal.hpp"
@@ -71,7 +82,7 @@ struct alignas(16) WaveMemory {
   uint32_t ksc[kUnit];                             // scale bytes of the keys
   uint32_t vsc[NH == 1 ? 1 : kUnit];               // ... of the values (one head: a lane has its own row's)
   float ks[NH == 1 ? 1 : kUnit];                   // 1, or NaN for a key that is; -1 without a row
-  float win_ks[NH == 1 ? 1 : kUnit];                             // window rows: the largest of the key's scales
+  float win_ks[NH == 1 ? 1 : kUnit];               // window rows: the largest of the key's scales
   float alpha[8];
 };
 
@@ -438,8 +449,9 @@ __global__ __launch_bounds__(kWaves * 64, NH == 1 ? 4 : 2) void attn_kv4_kernel(
     return pc;
   };
 
-  // A wave has one unit in flight: the next one's rows are requested when a unit's keys have become products, and its values are in LDS.  Requests are made whether there is a next unit or not (then for the sequence's first row): the wait for what a unit
-  // needs would be one for all requests if it were not known how many come after it.
+  // A wave has one unit in flight: the next one's rows are requested when a unit's keys have become products, and its values are in LDS.
+  // Requests are made whether there is a next unit or not (then for the sequence's first row): the wait for what a unit needs would be one
+  // for all requests if it were not known how many come after it.
   float m[L::kHeads], l[L::kHeads];   // running maximum of a head, and the sum of the lane's own weights
   f32x4 o[8];
   i32x4 k[4], v[4];

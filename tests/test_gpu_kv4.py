@@ -1,10 +1,13 @@
 """The operators on a key/value cache in 4 bits (a2ats_kv4_append, a2ats_kv4_read, a2ats_sparse_attn_kv4) against plain float64
 forms, through the C ABI."""
 import math
+import os
+import re
 
 import pytest
 import torch
 
+import bench
 from paper_2502_12665_amd import binding as B
 from paper_2502_12665_amd import synth
 from tests import kv4_ref as F
@@ -186,6 +189,26 @@ def test_bounds_keep_what_is_not_finite():
     bd = c.cache.bounds[0, 0].cpu()[:4]
     want = F.bounds(c.k[0][0], 16)
     assert torch.isnan(bd[0, :, 7]).all() and torch.equal(torch.nan_to_num(bd.double(), nan=99.0), torch.nan_to_num(want, nan=99.0))
+
+
+def test_bounds_of_bfloat16_of_both_signs_and_not_finite():
+    """Zeros of both signs, the smallest and largest numbers, infinities; NaN of either sign, in a call or in one before, makes both bounds
+    of its dimension NaN."""
+    c = Case([48], 1, 1, 16, "bf16", seed=11)
+    k = c.k[0][0]
+    k[:, 0], k[:, 1] = k[:, 0].abs(), -k[:, 1].abs()
+    k[3, 2], k[4, 2], k[5, 3], k[6, 4] = math.inf, -math.inf, -math.inf, math.inf
+    k[:16, 5], k[16:, 5] = 0.0, -0.0
+    k[:, 6] = torch.tensor([1, -1, 3, -3] * 12, dtype=torch.int16).view(torch.bfloat16) * 1.0
+    k[7, 7], k[8, 7] = torch.finfo(torch.bfloat16).max, torch.finfo(torch.bfloat16).min
+    k[2, 8], k[18, 9] = math.nan, torch.tensor([-1], dtype=torch.int16).view(torch.bfloat16)[0]
+    for n in (9, 20, 48):
+        c.append([n])
+    torch.cuda.synchronize()
+    bd, want = c.cache.bounds[0, 0].cpu()[:3].double(), F.bounds(k, 16)
+    assert torch.isnan(bd[0, :, 8]).all() and torch.isnan(bd[1, :, 9]).all()
+    assert torch.isnan(bd).sum() == 4 + 6                   # (dimension 6 has NaN with the sign, 0xffff and 0xfffd, beside the least numbers)
+    assert torch.equal(torch.nan_to_num(bd, nan=99.0), torch.nan_to_num(want, nan=99.0))
 
 
 # ---------------------------------------------------------------------------------------------- read back
@@ -532,3 +555,74 @@ def test_a_pool_of_more_than_4_gib():
     sel = draw_sel(c, blk, False, 3, 20, 2, 99)
     got = run_attend(c, sel, blk, False, 20, 2)
     check_attend(c, *got, sel, blk, False, 20, 2)
+
+
+# ---------------------------------------------------------------------------------------------- steps
+
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("ctx", [1024, 1003])
+def test_steps_of_the_benchmark(shared, ctx):
+    """Through the last block twice and a half: the cache holds the sequence up to each step's token, and its selection and output are those
+    of that sequence."""
+    wl = synth.WORKLOADS["c1_tiny"].replace(batch=2, ctx_len=ctx, top_k=96, window=40)
+    run = bench.BlockCacheSteps(torch, B, synth, wl, "e2m1", shared)
+    x = synth.make_decode_inputs(wl, device="cuda")
+    k, v, q = (x[c].cpu() for c in ("k", "v", "q"))
+    st, c = run.state, run.cache
+    cos_w, sin_w = st.cos_win.cpu().double(), st.sin_win.cpu().double()
+    for i in range(run.tokens * 5 // 2):
+        out = run.step(i)
+        n = run.first + i % run.tokens + 1
+        if i % run.tokens not in (0, 1, 9, run.tokens - 1):
+            continue
+        torch.cuda.synchronize()
+        for b in range(2):
+            rows, scales, kk, vv = F.cached(k[b, 0, :n], v[b, 0, :n])
+            assert torch.equal(c.rows[b, 0, :n].cpu(), rows) and torch.equal(c.scales[b, 0, :n].cpu(), scales)
+            bd = F.bounds(k[b, 0, :n], 16)
+            assert torch.equal(c.bounds[b, 0].cpu().double()[: -(-n // 16)], bd)
+            q_rot = st.q_rot[b].cpu().double()
+            picked = R.select(q_rot, bd, n, 16, 40, wl.n_sink, 6, shared)
+            for h in range(4):
+                blocks = picked[0 if shared else h][0]
+                assert st.block_idx[b, 0 if shared else h].tolist() == blocks
+                want, off = R.attend(q[b, h].double(), q_rot[h], kk, vv, n, R.tokens_of(blocks, n, 16, 40, wl.n_sink), 40, wl.n_sink, cos_w, sin_w)
+                half = HALF[st.out.dtype]
+                assert ((out[b, h].cpu().double() - want).abs() <= off * (1 + half) + half * want.abs()).all(), (i, b, h)
+
+
+def test_the_readme_program():
+    """README.md's code blocks as they stand, behind each other: after 20 tokens of a model with norms the cache holds the prompt's normalised
+    keys, and the last output is the attention of what was selected."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    code = "\n".join(re.findall(r"```python\n(.*?)```", open(os.path.join(root, "README.md")).read(), re.S))
+    at = code.index("# or blocks selected")
+    env = {}
+    exec(code[:at], env)
+    wl, x = env["wl"], env["x"]
+    N, w, G = wl.ctx_len, wl.window, wl.n_q_heads // wl.n_kv_heads
+    g = gen(2)
+    new = [[torch.randn(1, n, D, generator=g).bfloat16() for n in (wl.n_q_heads, wl.n_kv_heads, wl.n_kv_heads)] for _ in range(20)]
+    env["tokens"] = [(q.cuda(), k.unsqueeze(2).cuda(), v.unsqueeze(2).cuda()) for q, k, v in new]
+    exec(code[at:], env)
+    torch.cuda.synchronize()
+    n, bs, four = N + 20, env["bs4"], env["four"]
+    assert env["lens4"].tolist() == [n]
+    cos_w, sin_w = bs.cos_win.cpu().double(), bs.sin_win.cpu().double()
+    want_q = F.norm(new[-1][0].double(), env["q_weight"].cpu(), 1e-6)
+    assert ((bs.q_norm.cpu().double() - want_q).abs() <= F.half_step(want_q, torch.bfloat16) + 2 * F.NORM_ROUNDINGS * U * want_q.abs()).all()
+    back = [torch.empty(1, wl.n_kv_heads, n, D, device="cuda") for _ in range(2)]
+    B.kv4_read(env["grown"], four, n, env["lens4"], None, *back)
+    assert all(torch.equal(t[:, :, 20:], env[name]) for t, name in zip(back, ("k_back", "v_back")))
+    for h in (0, wl.n_q_heads - 1):
+        kv = h // G
+        rows, scales, k, v = F.cached(env["k_norm"][0, kv].cpu(), x["v"][0, kv].cpu())
+        assert torch.equal(four.rows[0, kv, :N].cpu(), rows) and torch.equal(four.scales[0, kv, :N].cpu(), scales)
+        kk, vv = (t[0, kv].cpu().double() for t in back)
+        assert torch.equal(kk[:N], k) and torch.equal(vv[:N], v)
+        blocks = bs.block_idx[0, h].tolist()
+        assert len(blocks) == wl.top_k // 16 and min(blocks) >= 0
+        want, off = R.attend(bs.q_norm[0, h].cpu().double(), bs.q_rot[0, h].cpu().double(), kk, vv, n, R.tokens_of(blocks, n, 16, w, 0), w, 0,
+                             cos_w, sin_w)
+        err = (env["out4"][0, h].cpu().double() - want).abs()
+        assert (err <= off * (1 + 2.0 ** -8) + 2.0 ** -8 * want.abs()).all(), (h, float(err.max()))
