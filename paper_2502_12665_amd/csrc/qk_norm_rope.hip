@@ -1,7 +1,7 @@
 // Norms of queries and keys, head by head, and their rotation by the tokens' positions, in one pass:
 //     y = x w / sqrt(mean(x^2) + eps),   y R_p,
-// each output rounded once, from float32.  Sums of squares are those of x 2^-e, |x| < 2 * 2^e, so that no square overflows; e >= -60,
-// so that eps 2^-2e does not either.
+// each output rounded once, from float32.  Where a sum of squares overflows, or is so small that squares are lost, it is that of
+// x 2^-e, |x| < 2 * 2^e; e >= -60, so that eps 2^-2e does not overflow either.
 //
 // A stream: 128 e bytes a head in, as many for each output.  16 lanes a row, a wave four rows at a time of one token, so that
 // the token's angles are loaded once for 16 heads; the other half of a rotated pair is eight lanes on.  Measured: 32768 tokens of 32 + 8 heads in
@@ -18,10 +18,24 @@ constexpr int kWaveHeads = 16;
 
 template <int CTRL>
 __device__ __forceinline__ uint32_t lane_of(uint32_t v) {
-  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false);
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
 }
 template <int CTRL>
 __device__ __forceinline__ float lane_of(float v) { return __uint_as_float(lane_of<CTRL>(__float_as_uint(v))); }
+// Over the 16 lanes of a row.
+template <typename T, typename F>
+__device__ __forceinline__ T over_row(T v, F f) {
+  v = f(v, lane_of<0xB1>(v));      // quad_perm [1,0,3,2]
+  v = f(v, lane_of<0x4E>(v));      // quad_perm [2,3,0,1]
+  v = f(v, lane_of<0x124>(v));     // row_ror:4
+  return f(v, lane_of<0x128>(v));  // row_ror:8
+}
+__device__ __forceinline__ float sum_of_squares(const float (&x)[8]) {
+  float sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sum += x[e] * x[e];
+  return over_row(sum, [](float a, float b) { return a + b; });
+}
 
 __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
   *(float4*)p = make_float4(x[0], x[1], x[2], x[3]);
@@ -40,7 +54,8 @@ __device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8]) {
 // Waves: [b][token][chunk of 16 heads]; the queries' heads before the keys'.
 template <typename T>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkNormArgs a, int batch, int Hq, int Hkv, int n_new, int ctx_len, int chunks) {
-  const uint32_t wave = blockIdx.x * 4 + (threadIdx.x >> 6), token = wave / (uint32_t)chunks;   // (fewer than 2^26)
+  const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+  const uint32_t token = wave / (uint32_t)chunks;   // (fewer than 2^26; rows of outputs fewer than 2^30)
   const int chunk = (int)(wave % (uint32_t)chunks), b = (int)(token / (uint32_t)n_new), t = (int)(token % (uint32_t)n_new);
   if (b >= batch) return;
   int n = a.seq_lens ? a.seq_lens[b] : ctx_len;
@@ -78,39 +93,41 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkNormArgs a, int bat
   for (int e = 0; e < 8; ++e) wq[e] = wk[e] = 1.f;
   if (a.q_weight) load8(a.q_weight + j * 8, wq);
   if (a.k_weight) load8(a.k_weight + j * 8, wk);
+  float w[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int h = h0 + i * 4 + slot;
-    uint32_t big = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) big = max(big, __float_as_uint(x[i][e]) & 0x7fffffffu);
-    big = max(big, lane_of<0xB1>(big));    // quad_perm [1,0,3,2]
-    big = max(big, lane_of<0x4E>(big));    // quad_perm [2,3,0,1]
-    big = max(big, lane_of<0x124>(big));   // row_ror:4
-    big = max(big, lane_of<0x128>(big));   // row_ror:8
-    const int e0 = min(max((int)(big >> 23) - 127, -60), 126);
-    const float down = __uint_as_float((uint32_t)(127 - e0) << 23);
-    float sum = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      x[i][e] *= down;
-      sum += x[i][e] * x[i][e];
-    }
-    sum += lane_of<0xB1>(sum);
-    sum += lane_of<0x4E>(sum);
-    sum += lane_of<0x124>(sum);
-    sum += lane_of<0x128>(sum);
-    const float r = rsqrtf(sum * (1.f / D) + ldexpf(a.eps, -2 * e0));
     const bool query = h < Hq;
+    if (i == 0 || (h0 + i * 4 + 3 >= Hq && h0 + i * 4 - 4 < Hq)) {   // (uniform; else they are those of the heads before)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = query ? wq[e] : wk[e];
+    }
+    float sum = sum_of_squares(x[i]), eps = a.eps;
+    // Squares that are lost below 2^-126 are below 2^-59 of such a sum, or of such an eps.
+    const bool far = !(sum < 0x1p126f) || (sum < 0x1p-60f && eps < 0x1p-60f);
+    if (__builtin_amdgcn_ballot_w64(far)) {
+      uint32_t big = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) big = max(big, __float_as_uint(x[i][e]) & 0x7fffffffu);
+      big = over_row(big, [](uint32_t p, uint32_t q) { return max(p, q); });
+      const int e0 = far ? min(max((int)(big >> 23) - 127, -60), 126) : 0;
+      const float down = __uint_as_float((uint32_t)(127 - e0) << 23);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[i][e] *= down;
+      sum = sum_of_squares(x[i]);
+      eps = ldexpf(eps, -2 * e0);
+    }
+    const float r = rsqrtf(sum * (1.f / D) + eps);
     float y[8], z[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = x[i][e] * r * (query ? wq[e] : wk[e]);
+    for (int e = 0; e < 8; ++e) y[e] = x[i][e] * r * w[e];
     if (turn) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] = y[e] * cs[e] + lane_of<0x128>(y[e]) * sn[e];
+      for (int e = 0; e < 8; ++e) z[e] = lane_of<0x128>(y[e]) * sn[e] + y[e] * cs[e];
     }
     if (h < last) {
-      const size_t to = (query ? (((size_t)b * Hq + h) * n_new + t) : (((size_t)b * Hkv + h - Hq) * n_new + t)) * D + j * 8;
+      const uint32_t row = (uint32_t)(query ? b * Hq + h : b * Hkv + h - Hq) * (uint32_t)n_new + (uint32_t)t;
+      const size_t to = (size_t)row * D + j * 8;
       T* norm = (T*)(query ? a.q_norm : a.k_norm);
       T* pos = (T*)(query ? a.q_pos : a.k_pos);
       if (norm) store8(norm + to, y);
