@@ -539,10 +539,10 @@ __global__ __launch_bounds__(kWaves * 64, NH == 1 ? 4 : 2) void attn_kv4_kernel(
           const int delta = distance(t);
           dot[t] = turned_dot<NH>(k[t], wm.ksc[t * 16 + col], a.cos_win + (size_t)delta * (kD / 2), a.sin_win + (size_t)delta * (kD / 2), lane,
                                   s.in.queries);
-          // (of the query's row 4 * lane row: the terms of a head have the same)
-          dot[t] *= wm.win_ks[NH == 1 ? 0 : t * 16 + col];
+          // (of the query's row 4 * lane row: the terms of a head have the same; the factors first, which may be 2^125 and 2^-105)
+          const float ks = wm.win_ks[NH == 1 ? 0 : t * 16 + col];
           const float4 qs = *(const float4*)(s.in.queries.win_scale + 4 * lrow);
-          dot[t] = f32x4{dot[t][0] * qs.x, dot[t][1] * qs.y, dot[t][2] * qs.z, dot[t][3] * qs.w};
+          dot[t] = f32x4{dot[t][0] * (qs.x * ks), dot[t][1] * (qs.y * ks), dot[t][2] * (qs.z * ks), dot[t][3] * (qs.w * ks)};
         }
       }
     }

@@ -515,6 +515,22 @@ def test_keys_and_values_of_any_size(G, shared, window):
             assert ((got[b, h] - p @ v).abs() <= (2 * d + U) * (p @ v.abs())).all(), (b, h)
 
 
+@pytest.mark.parametrize("G, shared", [(1, False), (3, True), (7, True)])
+@pytest.mark.parametrize("small, large", [(2.0 ** -97, 2.0 ** 122), (2.0 ** 122, 2.0 ** -97)])
+def test_window_of_factors_far_apart(G, shared, small, large):
+    """Queries and window keys whose factors are at either end of float32, with logits between: 2^25 and a quarter of it, so that the
+    output is the first key's value."""
+    c = Case([8], G, 1, 16, "f32", seed=99, bounds=False)
+    c.inv = torch.zeros(64, dtype=torch.float64)
+    c.k[0] = torch.full((1, 8, D), 0.25 * large)
+    c.k[0][:, 5] = large
+    c.append(c.lens)
+    c.q = torch.full((1, G, D), small)
+    got = run_attend(c, [[[] for _ in range(1 if shared else G)]], 1, shared, 8, 0, q_rot=c.q)[0]
+    want = c.seq(0, 0)[3][5]
+    assert torch.equal(got[0].double(), want.expand(G, D))
+
+
 def test_lengths_outside_of_their_range_are_limited():
     """seq_lens below 0 and above ctx_len, new_lens below 0, above n_new and above the sequence's length: the nearest that can be."""
     c = Case([96, 96, 96, 96], 4, 2, 32, "bf16", seed=97)
