@@ -637,19 +637,16 @@ def sparse_attn_kv4(dims: Dims, cache: Kv4Cache, q, q_rot, sel_idx, sel_count, n
     _check(rc, "a2ats_sparse_attn_kv4")
 
 
-def _projected(dims: Dims, x: Optional[torch.Tensor], name: str, heads: int, n_new: int):
+def _projected(dims: Dims, x: torch.Tensor, name: str, heads: int, n_new: int):
     """Pointer and token stride of [B, n_new, heads * D] (or [B, n_new, heads, D]) whose tokens are one distance apart."""
-    if x is None:
-        return None, 0
-    D, shape = dims.head_dim, tuple(x.shape)
-    if shape not in ((dims.batch, n_new, heads * D), (dims.batch, n_new, heads, D)):
-        raise ValueError(f"{name} has shape {shape}, not {(dims.batch, n_new, heads * D)}")
-    s = x.stride()
+    B, D, s, four = dims.batch, dims.head_dim, x.stride(), x.dim() == 4
+    if x.shape != ((B, n_new, heads, D) if four else (B, n_new, heads * D)):
+        raise ValueError(f"{name} has shape {tuple(x.shape)}, not {(B, n_new, heads * D)}")
     # (the stride of an axis of length 1 says nothing)
-    if s[-1] != 1 or (x.dim() == 4 and heads > 1 and s[2] != D):
+    if s[-1] != 1 or (four and heads > 1 and s[2] != D):
         raise ValueError(f"{name}: the heads of a token lie behind each other")
-    stride = s[1] if n_new > 1 else (s[0] if dims.batch > 1 else heads * D)
-    if dims.batch > 1 and s[0] != n_new * stride:
+    stride = s[1] if n_new > 1 else (s[0] if B > 1 else heads * D)
+    if B > 1 and s[0] != n_new * stride:
         raise ValueError(f"{name}: all tokens are the same distance apart")
     return x.data_ptr(), stride
 
@@ -662,38 +659,41 @@ def qk_norm_rope(dims: Dims, q, k, n_new: int, q_weight, k_weight, eps: float, c
     some = q if q is not None else k
     if some is None:
         raise ValueError("neither q nor k")
-    dev = some.get_device()
+    dt, dev = some.dtype, some.get_device()
     if dev < 0:
         raise ValueError(f"the tensors are on {some.device}")
     if dev != torch.cuda.current_device():
         raise ValueError(f"the tensors are on {some.device}, the current device is {torch.cuda.current_device()}")
     code = _dtype_code(some)
-    B, D, n_pos = dims.batch, dims.head_dim, 0
-    for name, x in (("q", q), ("k", k)):
-        if x is not None and (x.dtype != some.dtype or x.device != some.device):
-            raise TypeError(f"{name} is {x.dtype} on {x.device}, not {some.dtype} on {some.device}")
-    on = _Like(some.device, dev)
-    if cos_pos is not None:
-        n_pos = cos_pos.shape[0]
-    n_q, n_k = B * dims.n_q_heads * n_new * D, B * dims.n_kv_heads * n_new * D
-    qp, qs = _projected(dims, q, "q", dims.n_q_heads, n_new)
-    kp, ks = _projected(dims, k, "k", dims.n_kv_heads, n_new)
+    if q is not None and k is not None and (k.dtype is not dt or k.get_device() != dev):
+        raise TypeError(f"k is {k.dtype} on {k.device}, not {dt} on {some.device}")
+    B, D, Hq, Hkv = dims.batch, dims.head_dim, dims.n_q_heads, dims.n_kv_heads
+    on = _Like(some, dev)
+    n_pos = 0 if cos_pos is None else cos_pos.shape[0]
+    n_q, n_k, n_cs, f32, i32 = B * Hq * n_new * D, B * Hkv * n_new * D, n_pos * (D // 2), torch.float32, torch.int32
+    qp, qs = (None, 0) if q is None else _projected(dims, q, "q", Hq, n_new)
+    kp, ks = (None, 0) if k is None else _projected(dims, k, "k", Hkv, n_new)
     rc = lib().a2ats_qk_norm_rope(ctypes.byref(dims), qp, qs, kp, ks, code, n_new,
-                                  _arg(on, q_weight, "q_weight", torch.float32, D), _arg(on, k_weight, "k_weight", torch.float32, D),
-                                  eps, _arg(on, cos_pos, "cos_pos", torch.float32, n_pos * (D // 2)),
-                                  _arg(on, sin_pos, "sin_pos", torch.float32, n_pos * (D // 2)), n_pos,
-                                  _arg(on, seq_lens, "seq_lens", torch.int32, B), _arg(on, new_lens, "new_lens", torch.int32, B),
-                                  _arg(on, q_norm, "q_norm", some.dtype, n_q), _arg(on, k_norm, "k_norm", some.dtype, n_k),
-                                  _arg(on, q_pos, "q_pos", some.dtype, n_q), _arg(on, k_pos, "k_pos", some.dtype, n_k),
+                                  _arg(on, q_weight, "q_weight", f32, D), _arg(on, k_weight, "k_weight", f32, D),
+                                  eps, _arg(on, cos_pos, "cos_pos", f32, n_cs), _arg(on, sin_pos, "sin_pos", f32, n_cs), n_pos,
+                                  _arg(on, seq_lens, "seq_lens", i32, B), _arg(on, new_lens, "new_lens", i32, B),
+                                  _arg(on, q_norm, "q_norm", dt, n_q), _arg(on, k_norm, "k_norm", dt, n_k),
+                                  _arg(on, q_pos, "q_pos", dt, n_q), _arg(on, k_pos, "k_pos", dt, n_k),
                                   torch._C._cuda_getCurrentRawStream(dev))
     _check(rc, "a2ats_qk_norm_rope")
 
 
 class _Like:
-    """A device that the tensors of a call are on."""
+    """The device of a call's tensors, for _arg."""
 
-    def __init__(self, device, index):
-        self.device, self.device_index = device, index
+    __slots__ = ("some", "device_index")
+
+    def __init__(self, some, index):
+        self.some, self.device_index = some, index
+
+    @property
+    def device(self):
+        return self.some.device
 
 
 def _ws_ptr(cache: KvBlocks, ws: Optional[torch.Tensor]):
