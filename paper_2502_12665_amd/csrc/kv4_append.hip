@@ -7,10 +7,12 @@
 //
 // Both are streams, 2 * 128 * e bytes against 136.  16 lanes have a row, eight elements each: a group's largest is two steps over
 // four lanes, and a wave stores whole rows of 64 bytes.  Keys and values have workgroups of their own (kv8_append.hip has them so, by which
-// a token of 16 sequences is twice as many workgroups).  Measured: append of 32768 tokens of 8 heads in bfloat16 43.8 us with bounds (170 MB,
-// 3.9 TB/s), 4 x 4 heads of 4099 tokens in float32 14.8 us (76 MB, 5.2 TB/s); a token of 16 x 8 heads 4.0 us, a launch.  bfloat16 is
-// rounded as it comes from memory, and its bounds are taken two at a time as whole numbers: as float32 it was 51.5 us.  Reading back 65536
-// tokens of 4 heads in bfloat16 35 us (170 MB, 4.9 TB/s), 4 x 4 heads of 4099 tokens in float32 14.5 us (5.2 TB/s).
+// a token of 16 sequences is twice as many workgroups).  Measured: append of 32768 tokens of 8 heads in bfloat16 33 us with bounds (170 MB,
+// 5.2 TB/s), 4 x 4 heads of 4099 tokens in float32 14.8 us (76 MB, 5.2 TB/s); a token of 16 x 8 heads 4.0 us, a launch.  bfloat16 is
+// rounded as it comes from memory, and its bounds are taken two at a time as whole numbers: as float32 it was 8 us more.  Reading back 65536
+// tokens of 4 heads in bfloat16 27 us (170 MB, 6.2 TB/s; 35 with outputs that stay in L2), 4 x 4 heads of 4099 tokens in float32 11 us.  Both at
+// a copy's rate: what is read once, and what is read back, passes the caches; the cache's own rows do not, 4 bytes a lane of two workgroups'
+// lines (7 us more).
 #include "internal.hpp"
 #include "kv_bounds.hpp"
 
@@ -62,8 +64,10 @@ template <>
 struct Eight<uint16_t> {
   uint32_t x[4];
   __device__ __forceinline__ void load(const uint16_t* p) {
-    const uint4 v = *(const uint4*)p;
-    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+    typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+    const u32x4 v = __builtin_nontemporal_load((const u32x4*)p);   // (read once)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = v[e];
   }
   __device__ __forceinline__ void zero() { x[0] = x[1] = x[2] = x[3] = 0u; }
   __device__ __forceinline__ uint32_t largest() const {   // (two at a time, 16 bits each)
@@ -285,31 +289,73 @@ __global__ __launch_bounds__(NW * 64) void kv4_append_kernel(Kv4Cache m, const T
   }
 }
 
-// The eight numbers of a word of codes times a scale.
-__device__ __forceinline__ void store_numbers(float* p, uint32_t w, float scale, bool bad) {
-  float x[8];
-#define A2ATS_PAIR(i)                                                             \
-  {                                                                               \
-    const auto f = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, i);         \
-    x[2 * i] = f[0];                                                              \
-    x[2 * i + 1] = f[1];                                                          \
+// What 16 lanes have of a row that is read back, and how they store its numbers: 16 bytes a lane, all of them behind each other, past the
+// caches (a launch does not end before what it left in L2 is written).
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+template <typename T>
+struct ReadRow;
+// bfloat16: lane j the dimensions 8 j + 0 .. 7, of group j / 4: a word of the key's codes, and the value's bytes n = 4 (j % 4) + 0 .. 3 of all groups.
+template <>
+struct ReadRow<uint16_t> {
+  uint32_t k;
+  uint4 v;
+  uint2 sc;
+  __device__ __forceinline__ void load(const uint8_t* row, const uint8_t* scales, int j) {
+    k = *(const uint32_t*)(row + j * 4);
+    v = *(const uint4*)(row + kKv4Half + (j & 3) * 16);
+    sc = *(const uint2*)scales;
   }
-  A2ATS_PAIR(0) A2ATS_PAIR(1) A2ATS_PAIR(2) A2ATS_PAIR(3)
-#undef A2ATS_PAIR
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = bad ? __uint_as_float(0x7fc00000u) : x[i];
-  *(float4*)p = make_float4(x[0], x[1], x[2], x[3]);
-  *(float4*)(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
-}
-__device__ __forceinline__ void store_numbers(uint16_t* p, uint32_t w, float scale, bool bad) {
-  uint32_t x[4];
+  static __device__ __forceinline__ void put(uint16_t* to, int j, uint32_t w, uint32_t byte) {
+    const float scale = kv4_scale(byte);
+    u32x4 x;
 #define A2ATS_PAIR(i) x[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, i));
-  A2ATS_PAIR(0) A2ATS_PAIR(1) A2ATS_PAIR(2) A2ATS_PAIR(3)
+    A2ATS_PAIR(0) A2ATS_PAIR(1) A2ATS_PAIR(2) A2ATS_PAIR(3)
 #undef A2ATS_PAIR
 #pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = bad ? 0x7fc07fc0u : x[i];
-  *(uint4*)p = make_uint4(x[0], x[1], x[2], x[3]);
-}
+    for (int i = 0; i < 4; ++i) x[i] = byte == 255u ? 0x7fc07fc0u : x[i];
+    __builtin_nontemporal_store(x, (u32x4*)(to + j * 8));
+  }
+  __device__ __forceinline__ void key(uint16_t* to, int j) const { put(to, j, k, (sc.x >> (8 * (j >> 2))) & 255u); }
+  __device__ __forceinline__ void value(uint16_t* to, int j) const {
+    const int g = j >> 2;
+    const uint32_t pick = 0x0c0c0000u | (uint32_t)(4 + g) << 8 | (uint32_t)g;
+    const uint32_t lower = __builtin_amdgcn_perm(v.y, v.x, pick), upper = __builtin_amdgcn_perm(v.w, v.z, pick);
+    put(to, j, lower | upper << 16, (sc.y >> (8 * g)) & 255u);
+  }
+};
+// float32: lane j the dimensions 4 j + 0 .. 3 and 64 + 4 j + 0 .. 3, of the groups j / 8 and 2 + j / 8: half of two words of the key's codes, and
+// the value's bytes n = 2 (j % 8) + {0, 1} of all groups.
+template <>
+struct ReadRow<float> {
+  uint32_t k[2];
+  uint2 v, sc;
+  __device__ __forceinline__ void load(const uint8_t* row, const uint8_t* scales, int j) {
+    k[0] = *(const uint16_t*)(row + j * 2);
+    k[1] = *(const uint16_t*)(row + 32 + j * 2);
+    v = *(const uint2*)(row + kKv4Half + (j & 7) * 8);
+    sc = *(const uint2*)scales;
+  }
+  static __device__ __forceinline__ void put(float* to, uint32_t w, uint32_t byte) {
+    const float scale = kv4_scale(byte);
+    const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1);
+    f32x4 x = {a[0], a[1], b[0], b[1]};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = byte == 255u ? __uint_as_float(0x7fc00000u) : x[i];
+    __builtin_nontemporal_store(x, (f32x4*)to);
+  }
+  __device__ __forceinline__ void key(float* to, int j) const {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) put(to + 64 * h + 4 * j, k[h], (sc.x >> (16 * h + 8 * (j >> 3))) & 255u);
+  }
+  __device__ __forceinline__ void value(float* to, int j) const {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int g = 2 * h + (j >> 3);
+      put(to + 64 * h + 4 * j, __builtin_amdgcn_perm(v.y, v.x, 0x0c0c0000u | (uint32_t)(4 + g) << 8 | (uint32_t)g), (sc.y >> (8 * g)) & 255u);
+    }
+  }
+};
 
 // A wave has 16 rows, 16 lanes a row.
 template <typename T>
@@ -325,32 +371,22 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Cache m, int n_rows, i
   const int start = n - cnt, shift = m.at.shift;
   const int tid = threadIdx.x, lane = tid & 63, slot = lane >> 4, j = lane & 15;
   const int t0 = part * kKv4ReadRows + (tid >> 6) * 16;
-  uint32_t kw[4];
-  uint4 vw[4];
-  uint2 sc[4];
+  ReadRow<T> x[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int t = t0 + i * 4 + slot;
     if (t >= cnt) continue;
     const int row = start + t;
     const size_t r = (block_at(m.at, b, kv, row >> shift) << shift) + (size_t)(row & ((1 << shift) - 1));
-    kw[i] = *(const uint32_t*)(m.rows + r * kKv4RowBytes + j * 4);
-    vw[i] = *(const uint4*)(m.rows + r * kKv4RowBytes + kKv4Half + (j & 3) * 16);
-    sc[i] = *(const uint2*)(m.scales + r * kKv4ScaleBytes);
+    x[i].load(m.rows + r * kKv4RowBytes, m.scales + r * kKv4ScaleBytes, j);
   }
-  const int g = j >> 2;
-  const uint32_t pick = 0x0c0c0000u | (uint32_t)(4 + g) << 8 | (uint32_t)g;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int t = t0 + i * 4 + slot;
     if (t >= cnt) continue;
-    const size_t to = ((size_t)bh * n_rows + t) * D + j * 8;
-    const uint32_t kb = (sc[i].x >> (8 * g)) & 255u, vb = (sc[i].y >> (8 * g)) & 255u;
-    if (k_out) store_numbers(k_out + to, kw[i], kv4_scale(kb), kb == 255u);
-    if (v_out) {
-      const uint32_t lower = __builtin_amdgcn_perm(vw[i].y, vw[i].x, pick), upper = __builtin_amdgcn_perm(vw[i].w, vw[i].z, pick);
-      store_numbers(v_out + to, lower | upper << 16, kv4_scale(vb), vb == 255u);
-    }
+    const size_t to = ((size_t)bh * n_rows + t) * D;
+    if (k_out) x[i].key(k_out + to, j);
+    if (v_out) x[i].value(v_out + to, j);
   }
 }
 

@@ -4,9 +4,9 @@
 // x 2^-e, |x| < 2 * 2^e; e >= -60, so that eps 2^-2e does not overflow either.
 //
 // A stream: 128 e bytes a head in, as many for each output.  16 lanes a row, a wave four rows at a time of one token, so that
-// the token's angles are loaded once for 16 heads; the other half of a rotated pair is eight lanes on.  Measured: 32768 tokens of 32 + 8 heads in
-// bfloat16 with q_pos, k_norm and k_pos 163 us (755 MB, 4.6 TB/s); 4 x 1021 tokens of 28 + 4 heads in float32 20 us (87 MB, in
-// part from the caches); a token of 16 sequences 3.9 us, a launch.
+// the token's angles are loaded once for 16 heads.  Measured: 32768 tokens of 32 + 8 heads in bfloat16 with q_pos, k_norm and k_pos
+// 146 us (755 MB, 5.2 TB/s; 159 with outputs that stay in L2, 163 with all squares scaled); 4 x 1021 tokens of 28 + 4 heads in float32
+// 15 us (87 MB, in part from the caches; 20 with 32 bytes of a row a lane, which are half lines at a time); a token of 16 sequences 4.0 us, a launch.
 #include "internal.hpp"
 #include "kv_blocks.hpp"
 
@@ -37,19 +37,53 @@ __device__ __forceinline__ float sum_of_squares(const float (&x)[8]) {
   return over_row(sum, [](float a, float b) { return a + b; });
 }
 
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
-  *(float4*)p = make_float4(x[0], x[1], x[2], x[3]);
-  *(float4*)(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
-}
-__device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8]) {
-  typedef __attribute__((ext_vector_type(2))) float f32x2;
-  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-  uint32_t w[4];
+// Eight elements of a row's 16 lanes, which are loaded and stored 16 bytes a lane, all of them behind each other: bfloat16 8 j + 0 .. 7, the other half of
+// a rotated pair is eight lanes on; float32 4 j + 0 .. 3 and 64 + 4 j + 0 .. 3, the pair in one lane.  Outputs go past the caches: a launch
+// does not end before what it left in L2 is written.
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+template <typename T>
+struct Eight;
+template <>
+struct Eight<uint16_t> {
+  template <typename U>
+  static __device__ __forceinline__ void load(const U* row, int j, float (&x)[8]) { load8(row + j * 8, x); }
+  // The angles' cos and sin, with the sign of the other half.
+  static __device__ __forceinline__ void angles(const float* c, const float* s, int j, float (&cs)[8], float (&sn)[8]) {
+    load8(c + (j & 7) * 8, cs);
+    load8(s + (j & 7) * 8, sn);
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){x[2 * i], x[2 * i + 1]}, bf16x2));   // (to the nearest)
-  *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
-}
+    for (int e = 0; e < 8; ++e) sn[e] = j < 8 ? -sn[e] : sn[e];
+  }
+  static __device__ __forceinline__ float other_half(const float (&y)[8], int e) { return lane_of<0x128>(y[e]); }
+  static __device__ __forceinline__ void store(uint16_t* row, int j, const float (&x)[8]) {
+    typedef __attribute__((ext_vector_type(2))) float f32x2;
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){x[2 * i], x[2 * i + 1]}, bf16x2));   // (to the nearest)
+    __builtin_nontemporal_store(w, (u32x4*)(row + j * 8));
+  }
+};
+template <>
+struct Eight<float> {
+  static __device__ __forceinline__ void load(const float* row, int j, float (&x)[8]) {
+    const f32x4 a = *(const f32x4*)(row + j * 4), b = *(const f32x4*)(row + 64 + j * 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { x[e] = a[e]; x[e + 4] = b[e]; }
+  }
+  static __device__ __forceinline__ void angles(const float* c, const float* s, int j, float (&cs)[8], float (&sn)[8]) {
+    const f32x4 a = *(const f32x4*)(c + j * 4), b = *(const f32x4*)(s + j * 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { cs[e] = cs[e + 4] = a[e]; sn[e] = -b[e]; sn[e + 4] = b[e]; }
+  }
+  static __device__ __forceinline__ float other_half(const float (&y)[8], int e) { return y[e ^ 4]; }
+  static __device__ __forceinline__ void store(float* row, int j, const float (&x)[8]) {
+    __builtin_nontemporal_store(f32x4{x[0], x[1], x[2], x[3]}, (f32x4*)(row + j * 4));
+    __builtin_nontemporal_store(f32x4{x[4], x[5], x[6], x[7]}, (f32x4*)(row + 64 + j * 4));
+  }
+};
 
 // Waves: [b][token][chunk of 16 heads]; the queries' heads before the keys'.
 template <typename T>
@@ -76,23 +110,20 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkNormArgs a, int bat
     if (h < last) {
       const T* from = h < Hq ? (const T*)a.q + (size_t)token * a.q_stride + (size_t)h * D
                              : (const T*)a.k + (size_t)token * a.k_stride + (size_t)(h - Hq) * D;
-      load8(from + j * 8, x[i]);
+      Eight<T>::load(from, j, x[i]);
     }
   }
   const bool turn = a.q_pos != nullptr || a.k_pos != nullptr;
   float cs[8], sn[8];
   if (turn) {
-    const size_t at = (size_t)(n - cnt + t) * (D / 2) + (j & 7) * 8;
-    load8(a.cos_pos + at, cs);
-    load8(a.sin_pos + at, sn);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sn[e] = j < 8 ? -sn[e] : sn[e];
+    const size_t at = (size_t)(n - cnt + t) * (D / 2);
+    Eight<T>::angles(a.cos_pos + at, a.sin_pos + at, j, cs, sn);
   }
   float wq[8], wk[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) wq[e] = wk[e] = 1.f;
-  if (a.q_weight) load8(a.q_weight + j * 8, wq);
-  if (a.k_weight) load8(a.k_weight + j * 8, wk);
+  if (a.q_weight) Eight<T>::load(a.q_weight, j, wq);
+  if (a.k_weight) Eight<T>::load(a.k_weight, j, wk);
   float w[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -123,15 +154,15 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkNormArgs a, int bat
     for (int e = 0; e < 8; ++e) y[e] = x[i][e] * r * w[e];
     if (turn) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] = lane_of<0x128>(y[e]) * sn[e] + y[e] * cs[e];
+      for (int e = 0; e < 8; ++e) z[e] = Eight<T>::other_half(y, e) * sn[e] + y[e] * cs[e];
     }
     if (h < last) {
       const uint32_t row = (uint32_t)(query ? b * Hq + h : b * Hkv + h - Hq) * (uint32_t)n_new + (uint32_t)t;
-      const size_t to = (size_t)row * D + j * 8;
+      const size_t to = (size_t)row * D;
       T* norm = (T*)(query ? a.q_norm : a.k_norm);
       T* pos = (T*)(query ? a.q_pos : a.k_pos);
-      if (norm) store8(norm + to, y);
-      if (pos) store8(pos + to, z);
+      if (norm) Eight<T>::store(norm + to, j, y);
+      if (pos) Eight<T>::store(pos + to, j, z);
     }
   }
 }
