@@ -352,6 +352,35 @@ def test_attention_shared_out_or_not(batch, heads, kv_heads, n, n_sel, shared):
     assert torch.equal(got[0], again[0])                    # the workspace's contents do not matter, nor the run
 
 
+@pytest.mark.parametrize("shared", [False, True])
+def test_graphs_with_one_workspace(shared):
+    """Two captured calls of several workgroups a head that have one workspace, replayed in turn with other calls in it between."""
+    cases = [Case([900], 4, 1, 16, dtype, seed=63 + i, bounds=False) for i, dtype in enumerate(("f32", "bf16"))]
+    graphs, ws, side = [], torch.empty(1 << 20, dtype=torch.uint8, device="cuda"), torch.cuda.Stream()
+    for c in cases:
+        c.append(c.lens)
+        sel = draw_sel(c, 1, shared, 800, 40, 2, 65)
+        want, q_rot, cos_w, sin_w = run_attend(c, sel, 1, shared, 40, 2)           # (the kernels are loaded before the capture)
+        need = B.workspace_bytes(c.dims, B.OP_ATTN_KV4, 800, 40)
+        assert 4 * 130 * 4 * 2 <= need <= ws.numel()                               # (two parts at least)
+        args = [c.q.cuda(), q_rot.cuda(), torch.tensor(sel, dtype=torch.int32, device="cuda"),
+                torch.full((1, 1 if shared else 4), 800, dtype=torch.int32, device="cuda"), 800, 1, shared, 40, 2, cos_w.float().cuda(),
+                sin_w.float().cuda(), torch.tensor([900], dtype=torch.int32, device="cuda")]
+        out = torch.empty(1, 4, D, dtype=c.dtype, device="cuda")
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            B.sparse_attn_kv4(c.dims, c.cache, *args, out, ws)
+        graphs.append((graph, out, want, args))
+    for _ in range(4):
+        for graph, out, want, _ in graphs:
+            out.fill_(9.0)
+            ws.fill_(0xFF)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out.cpu(), want)
+
+
 @pytest.mark.parametrize("shared, heads", [(False, 6), (True, 6), (True, 16)])
 def test_what_is_not_attended(shared, heads):
     """Indices outside of the candidates, below zero and beyond the sequence, and counts outside of their range: left out; nothing attended: zeros, also for

@@ -127,6 +127,22 @@ def test_rows_that_are_not_finite():
         assert torch.equal(got[x], clean[x])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_do_not_depend_on_their_neighbours(dtype):
+    """Heads of a token beside others whose squares overflow, vanish or are not finite: the same bits as alone."""
+    dims, g = B.make_dims(1, 16, 4, D, 16, 64, 64), gen(41)
+    w = 1 + 0.2 * torch.randn(D, generator=g)
+    x = torch.randn(1, 6, 20, D, generator=g).to(DT[dtype])
+    y, at = x.clone(), torch.arange(20) % 4
+    for head, scale in ((1, 2.0 ** 90), (2, 2.0 ** -90), (3, math.nan)):
+        y[:, :, at == head] *= scale
+    for eps in (1e-6, 2.0 ** -126):
+        alone, beside = (run(dims, t[:, :, :16], t[:, :, 16:], 6, w, w, eps, [40], None)[0] for t in (x.cuda(), y.cuda()))
+        for name, o in alone.items():
+            assert torch.equal(o[:, 0::4], beside[name][:, 0::4]), name
+            assert beside[name][:, 3::4].isnan().all()
+
+
 def test_norms_over_32_bits_of_elements():
     """A projection of more than 2^31 elements, of which the last tokens are taken: offsets of 64 bits."""
     n, wide = 70000, 40 * D * 8                            # 2.9e9 bfloat16 elements
