@@ -38,7 +38,7 @@ __device__ __forceinline__ float sum_of_squares(const float (&x)[8]) {
 }
 
 // Eight elements of a row's 16 lanes, which are loaded and stored 16 bytes a lane, all of them behind each other: bfloat16 8 j + 0 .. 7, the other half of
-// a rotated pair is eight lanes on; float32 4 j + 0 .. 3 and 64 + 4 j + 0 .. 3, the pair in one lane.  Outputs go past the caches: a launch
+// a rotated pair is eight lanes on; float32 4 j + 0 .. 3 and 64 + 4 j + 0 .. 3, the pair in one lane.  Outputs go past the caches: probably a launch
 // does not end before what it left in L2 is written.
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
