@@ -646,7 +646,7 @@ def _projected(dims: Dims, x: torch.Tensor, name: str, heads: int, n_new: int):
     if s[-1] != 1 or (four and heads > 1 and s[2] != D):
         raise ValueError(f"{name}: the heads of a token lie behind each other")
     stride = s[1] if n_new > 1 else (s[0] if B > 1 else heads * D)
-    if B > 1 and s[0] != n_new * stride:
+    if B > 1 and n_new > 0 and s[0] != n_new * stride:
         raise ValueError(f"{name}: all tokens are the same distance apart")
     return x.data_ptr(), stride
 
