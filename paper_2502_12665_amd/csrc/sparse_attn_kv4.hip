@@ -82,7 +82,7 @@ struct alignas(16) WaveMemory {
   uint32_t ksc[kUnit];                             // scale bytes of the keys
   uint32_t vsc[NH == 1 ? 1 : kUnit];               // ... of the values (one head: a lane has its own row's)
   float ks[NH == 1 ? 1 : kUnit];                   // 1, or NaN for a key that is; -1 without a row
-  float win_ks[NH == 1 ? 1 : kUnit];               // window rows: the largest of the key's scales
+  int32_t win_exp[NH == 1 ? 1 : kUnit];            // window rows: the exponent of the largest of the key's scales
   float alpha[8];
 };
 
@@ -93,7 +93,7 @@ struct alignas(16) Queries {
   uint4 far[4][64];
   uint4 third[NH == 8 ? 4 : 1][64];
   uint4 win[NH == 1 ? 1 : 4][64];
-  float win_scale[64];
+  int32_t win_exp[64];
   float win_query[kD];   // one head
 };
 
@@ -155,7 +155,8 @@ __device__ __forceinline__ void put_win_queries(const T* from, int i, bool activ
   }
   big = rows_max(big) * kLogit;
   const int e0 = max((int)(__float_as_uint(big) >> 23) - 126, -97);
-  const float down = ldexpf(active && term < 3 ? 1.f : 0.f, 8 - e0);
+  // (an infinite element makes all of its head's terms NaN)
+  const float down = big < INFINITY ? ldexpf(active && term < 3 ? 1.f : 0.f, 8 - e0) : __uint_as_float(0x7fc00000u);
   const float less1 = term >= 1 ? 1.f : 0.f, less2 = term >= 2 ? 1.f : 0.f;
   float y[8];
   load8(from + at + 16 * (i & 1) + kD / 2 * (i >> 1), y);
@@ -168,7 +169,7 @@ __device__ __forceinline__ void put_win_queries(const T* from, int i, bool activ
     q[e] = (_Float16)z;
   }
   to.win[i][lane] = __builtin_bit_cast(uint4, q);
-  if (i == 0) to.win_scale[lane] = big < INFINITY ? ldexpf(1.f, e0 - 8) : __uint_as_float(0x7fc00000u);
+  if (i == 0) to.win_exp[lane] = e0 - 8;
 }
 
 // Byte `at` of row r.  PAGED: of a pool, which may have more than 2^32 bytes; otherwise of a sequence and KV head, at most 2^20 rows.
@@ -497,7 +498,7 @@ __global__ __launch_bounds__(kWaves * 64, NH == 1 ? 4 : 2) void attn_kv4_kernel(
       wm.vsc[NH == 1 ? 0 : lane] = at.in ? at.sc.y : 0u;
       wm.ks[NH == 1 ? 0 : lane] = at.in ? ks : -1.f;
     }
-    if (NH != 1 && 4 * u < win_tiles) wm.win_ks[NH == 1 ? 0 : lane] = kv4_scale(most);
+    if (NH != 1 && 4 * u < win_tiles) wm.win_exp[NH == 1 ? 0 : lane] = (int)most - 127;
 #pragma unroll
     for (int t = 0; t < 4; ++t) wm.values[value_slot<NH>(t, col)][lrow] = v[t];
     wave_exchange();
@@ -539,10 +540,11 @@ __global__ __launch_bounds__(kWaves * 64, NH == 1 ? 4 : 2) void attn_kv4_kernel(
           const int delta = distance(t);
           dot[t] = turned_dot<NH>(k[t], wm.ksc[t * 16 + col], a.cos_win + (size_t)delta * (kD / 2), a.sin_win + (size_t)delta * (kD / 2), lane,
                                   s.in.queries);
-          // (of the query's row 4 * lane row: the terms of a head have the same; the factors first, which may be 2^125 and 2^-105)
-          const float ks = wm.win_ks[NH == 1 ? 0 : t * 16 + col];
-          const float4 qs = *(const float4*)(s.in.queries.win_scale + 4 * lrow);
-          dot[t] = f32x4{dot[t][0] * (qs.x * ks), dot[t][1] * (qs.y * ks), dot[t][2] * (qs.z * ks), dot[t][3] * (qs.w * ks)};
+          // (The query's row 4 * lane row: the terms of a head have the same.  By the sum of both exponents: as factors, of up to 2^125 and
+          // 2^120 or 2^-105, they would overflow ahead of the logit, also where this is 0.)
+          const int ke = wm.win_exp[NH == 1 ? 0 : t * 16 + col];
+          const int4 qe = *(const int4*)(s.in.queries.win_exp + 4 * lrow);
+          dot[t] = f32x4{ldexpf(dot[t][0], qe.x + ke), ldexpf(dot[t][1], qe.y + ke), ldexpf(dot[t][2], qe.z + ke), ldexpf(dot[t][3], qe.w + ke)};
         }
       }
     }
