@@ -271,9 +271,10 @@ __device__ __forceinline__ f32x4 turned_dot(const i32x4& k, uint32_t sc, const f
   return acc;
 }
 
-// One head: products of the query with a tile's window keys, turned by the row's angles, on the vector ALU: of a pair of elements,
-//   (q R) . k = cos (q_l k_l + q_u k_u) + sin (q_l k_u - q_u k_l),
-// six operations, where the terms of turned keys are twelve.  Angles of eight pairs:
+// One head: products of the query, turned by the row's angles, with a tile's window keys, on the vector ALU: of a pair of elements,
+//   (q R) . k = (q_l cos - q_u sin) k_l + (q_l sin + q_u cos) k_u,
+// six operations, where the terms of turned keys are twelve.  (The angles go to the query: products of elements that do not meet, as those of
+// a pair's two halves in the last token's row, may be beyond float32.)  Angles of eight pairs:
 struct Angles {
   float cs[8], sn[8];
   __device__ __forceinline__ void load(const float* cos_win, const float* sin_win, int delta, int lrow, int i) {
@@ -291,7 +292,7 @@ __device__ __forceinline__ float turned_part(const i32x4& k, int i, float s_lowe
     const auto ku = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(words[1], s_upper, e);            \
     _Pragma("unroll") for (int j = 0; j < 2; ++j) {                                            \
       const int x = 2 * e + j;                                                                 \
-      sum += a.cs[x] * (ql[x % 4] * kl[j] + qu[x % 4] * ku[j]) + a.sn[x] * (ql[x % 4] * ku[j] - qu[x % 4] * kl[j]); \
+      sum += (ql[x % 4] * a.cs[x] - qu[x % 4] * a.sn[x]) * kl[j] + (ql[x % 4] * a.sn[x] + qu[x % 4] * a.cs[x]) * ku[j]; \
     }                                                                                          \
   }
 #define A2ATS_FOUR(at, first, second)                                                          \

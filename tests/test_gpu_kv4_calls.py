@@ -21,7 +21,7 @@ def test_norms_of_no_tokens(batch):
     torch.cuda.synchronize()
 
 
-@pytest.mark.parametrize("G, shared", [(3, True), (7, True)])
+@pytest.mark.parametrize("G, shared", [(1, False), (4, False), (3, True), (7, True)])
 @pytest.mark.parametrize("q_at, k_at", [(5, 70), (5, 69), (69, 5), (100, 3)])
 def test_window_of_large_elements_that_do_not_meet(G, shared, q_at, k_at):
     """A query and keys of 2^100 each, in different elements, also in two of a pair that is not turned (the last token's never is): no
