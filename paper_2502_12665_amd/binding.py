@@ -774,7 +774,8 @@ class DecodeState:
 class BlockDecodeState:
     """Device buffers for decode steps over a KvBlocks cache or a Kv4Cache with bounds (allocation only; no arithmetic).  scores:
     whether a step leaves the selected blocks' scores in block_score (which the attention does not need).  q_weight, k_weight, eps:
-    of a model that normalises the heads of its queries and keys; a step then takes them as they come from the projections."""
+    of a model that normalises the heads of its queries and keys; a step then takes queries, keys and values as they come from the
+    projections, slices of one tensor too (values that are one are copied first)."""
 
     def __init__(self, dims: Dims, cache, top_blocks: int, window: int, n_sink: int, inv_freq: torch.Tensor,
                  wrope_b: int, shared: bool = False, scores: bool = True, q_weight=None, k_weight=None, eps: float = 1e-6):
@@ -797,6 +798,7 @@ class BlockDecodeState:
         if q_weight is not None:
             self.q_norm = torch.empty(B, Hq, D, dtype=cache.kv_dtype, device=dev)
             self.k_norm = torch.empty(B, Hkv, 1, D, dtype=cache.kv_dtype, device=dev)
+            self.v_new = torch.empty(B, Hkv, 1, D, dtype=cache.kv_dtype, device=dev)
         n_ws = max(workspace_bytes(dims, OP_BLOCK_TOPK),
                    workspace_bytes(dims, OP_ATTN_KV4 if self.four_bits else OP_ATTN_KV8, top_blocks * cache.block, window), 256)
         self.ws = torch.empty(n_ws, dtype=torch.uint8, device=dev)
@@ -812,6 +814,8 @@ class BlockDecodeState:
             qk_norm_rope(dims, q.reshape(dims.batch, 1, -1), k_new.reshape(dims.batch, 1, -1), 1, self.q_weight, self.k_weight, self.eps,
                          None, None, seq_lens, None, q_norm=self.q_norm, k_norm=self.k_norm)
             q, k_new = self.q_norm, self.k_norm
+            if not v_new.is_contiguous() and v_new.shape == self.v_new.shape and v_new.dtype == self.v_new.dtype and v_new.device == self.v_new.device:
+                v_new = self.v_new.copy_(v_new)            # (what does not fit is the append's to refuse)
         append(dims, self.cache, k_new, v_new, 1, seq_lens)
         block_topk(dims, self.blocks, q, self.cos_b, self.sin_b, self.q_rot, self.shared, self.top_blocks, self.window,
                    self.n_sink, seq_lens, self.block_idx, self.block_count, self.block_score, ws=self.ws)

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2502_12665_amd import binding as B
-from tests.test_gpu_kv4 import Case, run_attend
+from tests.test_gpu_kv4 import Case, gen, run_attend
 
 pytestmark = pytest.mark.gpu
 D = 128
@@ -36,3 +36,33 @@ def test_window_of_large_elements_that_do_not_meet(G, shared, q_at, k_at):
     got = run_attend(c, [[[] for _ in range(1 if shared else G)]], 1, shared, 8, 0, q_rot=c.q)[0]
     want = c.seq(0, 0)[3].mean(0)
     assert torch.equal(got[0].double(), want.expand(G, D))
+
+
+@pytest.mark.parametrize("four_bits", [True, False])
+def test_steps_of_packed_projections(four_bits):
+    """Queries, keys and values of a step as slices of one projection: the cache, the selection and the output are those of a step that is
+    given them contiguous."""
+    batch, heads, kv_heads = 3, 8, 2
+    dims = B.make_dims(batch, heads, kv_heads, D, 16, 100, 112)
+    inv = torch.exp(-torch.arange(64, dtype=torch.float64) / 8)
+    g = gen(102)
+    w = [(1 + 0.2 * torch.randn(D, generator=g)).cuda() for _ in range(2)]
+    states = []
+    for _ in range(2):
+        cache = (B.Kv4Cache if four_bits else B.KvBlocks).empty(dims, 16, torch.bfloat16)
+        cache.bounds.zero_()
+        states.append((cache, B.BlockDecodeState(dims, cache, 2, 20, 1, inv, 64, False, q_weight=w[0], k_weight=w[1])))
+    lens = torch.zeros(batch, dtype=torch.int32, device="cuda")
+    for i in range(40):
+        lens += 1
+        x = torch.randn(batch, heads + 2 * kv_heads, D, generator=g).bfloat16().cuda()
+        q, k, v = x[:, :heads], x[:, heads:heads + kv_heads].unsqueeze(2), x[:, heads + kv_heads:].unsqueeze(2)
+        outs = [states[0][1].step(q, k, v, lens), states[1][1].step(q.contiguous(), k.contiguous(), v.contiguous(), lens)]
+        assert torch.equal(*outs) and torch.equal(states[0][1].block_idx, states[1][1].block_idx), i
+    # (codes of 8 bits: of the two complete blocks, the others are not written)
+    for name, n in (("rows", 40), ("scales", 40)) if four_bits else (("k", 32), ("v", 32), ("k_scale", 2), ("v_scale", 2), ("v_tail", 16)):
+        assert torch.equal(*(getattr(s[0], name)[:, :, :n].contiguous().view(torch.uint8) for s in states)), name
+    assert torch.isfinite(outs[0]).all() and (outs[0] != 0).any()
+    for bad in (v.float(), v[:, :1], v.transpose(0, 1)):    # (neither converted nor spread)
+        with pytest.raises((TypeError, ValueError)):
+            states[0][1].step(q, k, bad, lens)
