@@ -705,38 +705,53 @@ __global__ __launch_bounds__(kWaves * 64, NH == 1 ? 4 : 2) void attn_kv4_kernel(
 
 }  // namespace
 
-// Parts: a second launch that joins them, 3 us, against units of 64 rows that a wave has to take one after the other, 1.5 us each (2.6 for
-// heads that share a selection) while there is a workgroup a CU at most.  So: the least parts that leave a wave the fewest units, with no more
-// workgroups than CUs, where that saves two units.  Measured for 2 to 896 problems of 160 to 4160 rows with 1 to 16 parts (bfloat16, window
+// The most parts that a head's (KV head's) rows are shared out to, whatever their number: as many workgroups as CUs, or two parts.
+static long most_parts(long problems) {
+  if (problems <= 128) return problems > 0 ? std::min(256 / problems, 12l) : 1;
+  return problems > 256 && (problems - 1) % 256 < 128 ? 2 : 1;
+}
+
+// Parts: a second launch that joins them, 3 us of a pass, against units of 64 rows that a wave has to take one after the other, 1.5 us each
+// (2.6 for heads that share a selection) while there is a workgroup a CU at most.  So: the least parts that leave a wave the fewest units, with no
+// more workgroups than CUs, where that saves two units.  (Units of selected rows and of the window: sinks are shared out with the selected rows but not
+// counted, as they are few.)  Measured for 2 to 896 problems of 160 to 4160 rows with 1 to 16 parts (bfloat16, window
 // 64), us with one part -> with the parts taken: 2 problems, 576 rows 10.1 -> 9.5 (3 parts), 2304 rows 18.1 -> 10.4 (12); 32 problems, 1152
 // rows 12.9 -> 10.0 (6), 4160 rows 28.5 -> 13.0 (6); 128 problems, 2304 rows 19.3 -> 17.1 (2; four: 18.5); 256 problems, 2304 rows would be
-// 20.2 -> 23.9; shared by four heads, 8 problems, 1152 rows 19.2 -> 12.4 (6), 128 problems, 1152 rows 20.4 -> 19.7 (2).  Many rows of problems
-// that leave half a round of CUs over: 896 problems, 4160 rows 102 -> 96 (2), 384 problems 48.1 -> 44.1, but with 2304 rows 61.7 -> 62.1.
+// 20.2 -> 23.9; shared by four heads, 8 problems, 1152 rows 19.2 -> 12.4 (6), 128 problems, 1152 rows 20.4 -> 19.7 (2).
+// More problems than CUs, of which half a round of CUs or less is left over: two parts make half a round of it, which pays for many rows, from 16 units a
+// wave on (shared selections, of which fewer workgroups are resident: 24).  One part -> two, problems of 4160 rows: 264 44.0 -> 45.3, 288 42.0 ->
+// 39.7, 376 46.9 -> 46.6, 384 42.1 -> 39.7, 520 74.3 -> 65.8, 640 62.0 -> 60.5, 784 95.1 -> 91.2, 896 85.1 -> 83.4, 1152 105 -> 107;
+// of 15256 rows: 288 124 -> 104, 520 222 -> 189, 896 262 -> 239, 1152 331 -> 303.  More than half a round left over, 4160 rows: 392 47.5 -> 56.3, 656 73.4
+// -> 76.3, 904 96 -> 102; 2304 rows: 384 28.3 -> 28.9, 896 53.1 -> 57.5.  Shared by four heads, 6064 rows: 264 74.5 -> 71.3, 520 124 -> 113, 640 133 -> 125, 896
+// 168 -> 172, by eight 208 -> 203; 4160 rows, four heads: 384 58.0 -> 59.7, 520 94.6 -> 90.1, 896 126 -> 136.
 Kv4Plan make_kv4_plan(const a2ats_dims& d, long sel_rows, int window, bool shared) {
-  const long problems = (long)d.batch * (shared ? d.n_kv_heads : d.n_q_heads);
+  const long problems = (long)d.batch * (shared ? d.n_kv_heads : d.n_q_heads), most = most_parts(problems);
   const long far = std::min<long>(sel_rows, d.ctx_len), win = std::min(window, d.ctx_len);
   auto units = [&](long parts) {
     const long f = (far + parts - 1) / parts, w = (win + parts - 1) / parts;
     return ((f + 16 * kWaves - 1) / (16 * kWaves) + (w + 16 * kWaves - 1) / (16 * kWaves) + 3) / 4;
   };
   long parts = 1;
-  for (long p = 2; p <= 12 && p * problems <= 256; ++p)
-    if (units(p) < units(parts)) parts = p;
-  if (units(1) - units(parts) < 2) parts = 1;
-  if (problems > 256 && problems % 256 == 128 && units(1) >= 16) parts = 2;
+  if (problems > 128) {
+    if (units(1) >= (shared && d.n_q_heads > d.n_kv_heads ? 24 : 16)) parts = most;
+  } else {
+    for (long p = 2; p <= most; ++p)
+      if (units(p) < units(parts)) parts = p;
+    if (units(1) - units(parts) < 2) parts = 1;
+  }
   Kv4Plan p;
   p.parts = (int)parts;
   p.bytes = parts > 1 ? (size_t)d.batch * d.n_q_heads * parts * (kD + 2) * sizeof(float) : 0;
   return p;
 }
 
-// What every call with at most so many selected tokens and such a window needs.
+// What every call with at most so many selected tokens and such a window needs.  (A plan of two parts or more has three units at least, which are more
+// than 4 * kUnit rows.)
 size_t kv4_ws_bytes(const a2ats_dims& d, long sel_rows, int window) {
   const long rows = std::min<long>(sel_rows, d.ctx_len) + std::min(window, d.ctx_len);
   size_t need = 0;
   for (int shared = 0; shared < 2; ++shared) {
-    const long problems = (long)d.batch * (shared ? d.n_kv_heads : d.n_q_heads);
-    const long parts = problems <= 128 ? std::min(problems > 0 ? 256 / problems : 1, 12l) : (problems > 256 && problems % 256 == 128 ? 2 : 1);
+    const long parts = most_parts((long)d.batch * (shared ? d.n_kv_heads : d.n_q_heads));
     if (parts > 1 && rows > 4 * kUnit) need = std::max(need, (size_t)d.batch * d.n_q_heads * parts * (kD + 2) * sizeof(float));
   }
   return need;

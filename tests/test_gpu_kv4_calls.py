@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2502_12665_amd import binding as B
-from tests.test_gpu_kv4 import Case, gen, run_attend
+from tests.test_gpu_kv4 import Case, check_attend, draw_sel, gen, run_attend
 
 pytestmark = pytest.mark.gpu
 D = 128
@@ -66,3 +66,33 @@ def test_steps_of_packed_projections(four_bits):
     for bad in (v.float(), v[:, :1], v.transpose(0, 1)):    # (neither converted nor spread)
         with pytest.raises((TypeError, ValueError)):
             states[0][1].step(q, k, bad, lens)
+
+
+def needs_parts(c, n_sel, size, shared, window):
+    """Whether the call is one of several workgroups a head: it is refused without a workspace."""
+    o = torch.zeros(c.batch, c.heads, D, dtype=c.dtype, device="cuda")
+    H = c.kv_heads if shared else c.heads
+    idx, cnt = (torch.zeros(c.batch, H, n, dtype=torch.int32, device="cuda") for n in (n_sel, 1))
+    tables = [torch.zeros(max(window, 1), D // 2, device="cuda")] * 2
+    if B.workspace_bytes(c.dims, B.OP_ATTN_KV4, n_sel * size, window) == 0:
+        return False
+    try:
+        B.sparse_attn_kv4(c.dims, c.cache, o, o.float(), idx, cnt, n_sel, size, shared, window, 0, *tables, None, torch.zeros_like(o), None)
+    except B.A2atsError as e:
+        assert "orkspace" in str(e), e
+        return True
+    return False
+
+
+@pytest.mark.parametrize("G, kv_heads, shared, unit, n_sel", [(4, 2, False, 1, 4096), (1, 8, False, 16, 260), (2, 8, True, 16, 380)])
+@pytest.mark.parametrize("page", [0, 32])
+def test_two_parts_of_many_heads(G, kv_heads, shared, unit, n_sel, page):
+    """More heads (KV heads) than compute units, half a round of them left over: two workgroups each."""
+    lens = [6300] + [17, 0, 300, 1, 65] * 7
+    c = Case(lens, kv_heads * G, kv_heads, 16, "bf16", page, seed=115, bounds=False)
+    assert 256 < c.batch * (kv_heads if shared else c.heads) <= 384
+    c.append(c.lens)
+    assert needs_parts(c, n_sel, unit, shared, 64)
+    sel = draw_sel(c, unit, shared, n_sel, 64, 2, 116)
+    got = run_attend(c, sel, unit, shared, 64, 2)
+    check_attend(c, *got, sel, unit, shared, 64, 2)
