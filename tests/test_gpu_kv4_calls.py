@@ -84,6 +84,21 @@ def needs_parts(c, n_sel, size, shared, window):
     return False
 
 
+@pytest.mark.parametrize("page", [0, 64])
+@pytest.mark.parametrize("unit, n_sel, window, n_sink", [(1, 1500, 100, 4), (32, 50, 300, 0), (1, 1024, 0, 1200)])
+@pytest.mark.parametrize("G, shared", [(1, False), (4, False), (8, False), (1, True), (3, True), (8, True)])
+def test_parts_of_ragged_batches(G, shared, unit, n_sel, window, n_sink, page):
+    """Several workgroups a head over sequences of 5000 tokens to none: parts without a row, selections split inside of a block, windows and
+    sinks past the sequence's end."""
+    c = Case([900, 5000, 70, 0, 1, 2100], 2 * G, 2, 32, "bf16" if G % 4 else "f32", page, seed=110 + G, bounds=False)
+    c.append(c.lens)
+    assert needs_parts(c, n_sel, unit, shared, window)
+    sel = draw_sel(c, unit, shared, n_sel, window, n_sink, 111)
+    got = run_attend(c, sel, unit, shared, window, n_sink)
+    check_attend(c, *got, sel, unit, shared, window, n_sink)
+    assert (got[0][3] == 0).all()
+
+
 @pytest.mark.parametrize("G, kv_heads, shared, unit, n_sel", [(4, 2, False, 1, 4096), (1, 8, False, 16, 260), (2, 8, True, 16, 380)])
 @pytest.mark.parametrize("page", [0, 32])
 def test_two_parts_of_many_heads(G, kv_heads, shared, unit, n_sel, page):
