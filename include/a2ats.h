@@ -564,7 +564,8 @@ int a2ats_kv4_read(const a2ats_dims* dims, const a2ats_kv4* cache, int32_t n_row
  * a2ats_sparse_attn_kv8 over a cache in 4 bits: arguments, attended set and results as there, every row code * scale.  Products,
  * sums and weights are those of float32 (queries, weights and keys enter their products whole; but for two heads or more of a shared
  * selection the turned keys of window rows are two float16 numbers, off by at most 2^-23 of each element and 2^-26 of the row's
- * largest, and for 5 to 8 heads the queries of window rows are too).  The block selection over such a cache is a2ats_block_topk,
+ * largest, and for 5 to 8 heads the queries of window rows are too); weights are those relative to the largest and divided by their sum
+ * last, so that their sums with values have to be float32 too (values times rows below 2^128).  The block selection over such a cache is a2ats_block_topk,
  * given its bounds, block, kv_dtype, page_table and page_size in an a2ats_kv_blocks.
  * Workspace: a2ats_workspace_bytes(dims, A2ATS_OP_ATTN_KV4, n_sel * sel_size, window).
  */

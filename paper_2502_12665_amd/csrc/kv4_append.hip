@@ -8,8 +8,8 @@
 // Both are streams, 2 * 128 * e bytes against 136.  16 lanes have a row, eight elements each: a group's largest is two steps over
 // four lanes, and a wave stores whole rows of 64 bytes.  Keys and values have workgroups of their own (kv8_append.hip has them so, by which
 // a token of 16 sequences is twice as many workgroups).  Measured: append of 32768 tokens of 8 heads in bfloat16 33 us with bounds (170 MB,
-// 5.2 TB/s), 4 x 4 heads of 4099 tokens in float32 14.8 us (76 MB, 5.2 TB/s); a token of 16 x 8 heads 4.0 us, a launch.  bfloat16 is
-// rounded as it comes from memory, and its bounds are taken two at a time as whole numbers: as float32 it was 8 us more.  Reading back 65536
+// 5.2 TB/s), 4 x 4 heads of 4099 tokens in float32 14.8 us (76 MB, 5.2 TB/s); a token of 16 x 8 heads 4.0 us: a launch, 1.6, and length -> rows.
+// bfloat16 is rounded as it comes from memory, and its bounds are taken two at a time as whole numbers: as float32 it was 8 us more.  Reading back 65536
 // tokens of 4 heads in bfloat16 27 us (170 MB, 6.2 TB/s; 35 with outputs that stay in L2), 4 x 4 heads of 4099 tokens in float32 11 us.  Both at
 // a copy's rate: what is read once, and what is read back, passes the caches; the cache's own rows do not, 4 bytes a lane of two workgroups'
 // lines (7 us more).

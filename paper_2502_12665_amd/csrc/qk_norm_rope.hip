@@ -6,7 +6,10 @@
 // A stream: 128 e bytes a head in, as many for each output.  16 lanes a row, a wave four rows at a time of one token, so that
 // the token's angles are loaded once for 16 heads.  Measured: 32768 tokens of 32 + 8 heads in bfloat16 with q_pos, k_norm and k_pos
 // 146 us (755 MB, 5.2 TB/s; 159 with outputs that stay in L2, 163 with all squares scaled); 4 x 1021 tokens of 28 + 4 heads in float32
-// 15 us (87 MB, in part from the caches; 20 with 32 bytes of a row a lane, which are half lines at a time); a token of 16 sequences 4.0 us, a launch.
+// 15 us (87 MB, in part from the caches; 20 with 32 bytes of a row a lane, which are half lines at a time); a token of 16 sequences 4.0 us: a launch,
+// 1.6, and length -> row -> root.  (All of a pass in a graph.  Single kernels as rocprofv3 has them: 147 us and more for the 146, 154 on average; 4.5
+// to 4.8 for the 4.0.)  32768 tokens of 8 + 1 heads 36 us and keys alone of 8 heads 27, a copy's rate; of 1 + 1 heads 23 against 12, as 14 of a wave's
+// 16 places have no row.
 #include "internal.hpp"
 #include "kv_blocks.hpp"
 

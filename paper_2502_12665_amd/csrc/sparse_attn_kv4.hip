@@ -27,7 +27,7 @@
 // TB/s of the 265 MB that they are); this kernel 60 us without a window and 72 us with 128 rows of window, whose angles, 64 KB for a
 // head, pass through the first-level cache.  A row's key and value are requested one after the other, as they are one line: by
 // tiles of keys and then tiles of values it took 67 us.  With few heads it is the latency of a unit (64 rows a wave, of which the next is
-// in flight): 4 x 32 heads of 2304 rows 16.5 us and 3 us to join their parts, 7.6 us at the rate of a copy.  Workgroups of 8 and 16 waves
+// in flight): 4 x 32 heads of 2304 rows 16.5 us and 3 us of a pass (4.1 to 4.7 by itself) to join their parts, 7.6 us at the rate of a copy.  Workgroups of 8 and 16 waves
 // instead of 4 take as long or longer at nearly all sizes (128 problems, 2304 rows 18.5 and 20.7 us against 19.4; 896 problems 60.8 with
 // four), two units in flight for each wave too.
 #include <algorithm>
